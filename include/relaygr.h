@@ -201,6 +201,50 @@ int  relaygr_kv_pool_stats(relaygr_kv_pool* pool, int64_t* pages_total, int64_t*
 int  relaygr_kv_pool_locate(relaygr_kv_pool* pool, relaygr_kv_handle handle, int32_t layer,
                             int32_t token, int32_t feature, int64_t* k_index, int64_t* v_index);
 
+/* ---- the same pool in 8 bits ------------------------------------------------------------ */
+
+/* K and V as e4m3 codes with one power-of-two scale for each block: the 64 tokens of a tile, of one head of K or of V, in
+ * one layer.  With a the largest finite magnitude of a block, e = floor(log2 a) - 8, one more if a > 1.75 * 2^floor(log2 a), and at
+ * least -100; a value x is held as the e4m3 number nearest to x / 2^e (ties to even) and stands for that number times 2^e: within 2^-4 of
+ * itself, or of 2^(e-6) where it is smaller.  Infinities and NaN are held as NaN (e4m3 has no infinity); values of more than 240/256 of the
+ * power of two behind the storage type's largest (bf16 2^128, fp16 65536) as +-240/256 of it.  For the 16-bit storage types
+ * (RELAYGR_DTYPE_BF16, RELAYGR_DTYPE_FP16), with half their bytes: twice the live caches in the same HBM, half the bytes of a spill or reload. */
+
+/* Bytes of psi for one user in 8 bits, scales included; what it occupies in a pool of such pages.  0 on bad input. */
+size_t relaygr_kv_footprint_bytes_q8(const relaygr_model_config* cfg, int32_t prefix_len);
+size_t relaygr_kv_pool_bytes_for_q8(const relaygr_model_config* cfg, int32_t prefix_len, int32_t page_tokens);
+/* relaygr_kv_pool_create for K and V in 8 bits.  A page holds page_tokens / 64 tiles of every layer's codes and scales
+ * (relaygr_kv_pool_bytes_for_q8).  Every relaygr_kv_pool_* and relaygr_expander_* call takes such a pool (relaygr_kv_pool_locate then counts in
+ * bytes, and says where codes are), and so do the three calls below. */
+int  relaygr_kv_pool_create_q8(const relaygr_model_config* cfg, void* slab_dev, size_t slab_bytes,
+                               int32_t page_tokens, relaygr_kv_pool** out);
+
+/* Rows of a batch of users.  HOST arrays; user u has the rows row_off[u] .. row_off[u+1]-1 of the call's device arrays. */
+typedef struct {
+  int32_t n_users;
+  const relaygr_kv_handle* handles;   /* [n_users] live entries */
+  const int32_t* row_off;             /* [n_users + 1], monotone, starting at 0 */
+  const int32_t* first_token;         /* [n_users] write, read: the entry's token that the user's first row is; null: 0 */
+  const int32_t* key_len;             /* [n_users] attend: tokens of the entry that take part, from its first on; null: all */
+} relaygr_kv_rows;
+
+/* The device arrays k, v, q and out hold one row of d_model elements (heads side by side) of the storage type for each row of the
+ * batch, `stride` elements from one to the next: at least d_model and a multiple of 8, the first row 16-byte aligned (a block of columns
+ * of a wider array is such an array).  They are read, or written, in hip_stream's order.  Errors of all three: RELAYGR_ENOENT for a
+ * handle that is not live, RELAYGR_EINVAL for tokens beyond an entry, a layer that the model does not have, rows that are not
+ * aligned, a pool that does not hold 8 bits; nothing is enqueued then.  Calls without users or rows are not errors.  Write and read
+ * take no context and no scratch: they may be captured into a graph, and several may run at once on different entries. */
+
+/* Quantises rows of one layer's K and V into the entries' tokens first_token[u] on, as a block's last tokens: tokens before first_token
+ * in the first block that is touched keep what they stand for, rounded again under the block's new scale where that makes them
+ * subnormal; the tokens behind the last row in its block become zero.  An entry is thus written front to back, in one call or in
+ * many, and a write into its middle ends it there.  RELAYGR_EINVAL if two users of the batch carry the same handle. */
+int  relaygr_kv_pool_write(relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, const void* k, int64_t k_stride,
+                           const void* v, int64_t v_stride, void* hip_stream);
+/* The values that tokens of the entries stand for, into rows of k and v. */
+int  relaygr_kv_pool_read(relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, void* k, int64_t k_stride,
+                          void* v, int64_t v_stride, void* hip_stream);
+
 /* ---- compute (Section 3.2: the instance dispatches on the request's stage) ------------ */
 
 /* stage = pre-infer.  For every user of the batch: run the backbone over prefix_emb rows of that
@@ -247,6 +291,16 @@ size_t relaygr_static_scratch_bytes(void);
  * and no pool is touched.  Same output as relaygr_rank_with_cache. */
 int  relaygr_rank_full_recompute(relaygr_ctx* ctx, const relaygr_batch* batch,
                                  float* scores_dev, void* hip_stream);
+
+/* One layer's attention over entries of an 8-bit pool, for backbones that bring their own projections: in the context's form,
+ *   out_i^h = (1/n_i) sum_{j < n_i} SiLU(alpha <q_i^h, k_j^h>) v_j^h    or    sum_{j < n_i} softmax_j(alpha <q_i^h, k_j^h>) v_j^h,
+ * alpha = 1 / sqrt(d_head), over the first n_i tokens of the user's entry: key_len[u] for every row, as candidates see a prefix, or, with
+ * causal != 0, for rows that are themselves the last of these tokens: row i of the user's n sees max(0, key_len[u] - n + 1 + i).  A row that sees
+ * nothing is zero.  NaN in K or V reaches the rows that see its token only.  out must not overlap q or the slab.  Uses the context's form, scratch and
+ * stream order (not its weights), so contexts' rules for streams, threads and graphs hold; rows are cut along the keys only as far as
+ * the scratch holds their partial sums, so any call fits. */
+int  relaygr_cache_attend(relaygr_ctx* ctx, relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, int32_t causal,
+                          const void* q, int64_t q_stride, void* out, int64_t out_stride, void* hip_stream);
 
 /* ---- measurement ---------------------------------------------------------------------- */
 

@@ -37,6 +37,8 @@ EXPORTS = [
     "relaygr_admission_budget_compute", "relaygr_slot_throughput",
     "relaygr_trigger_create", "relaygr_trigger_destroy", "relaygr_trigger_admit", "relaygr_trigger_release",
     "relaygr_trigger_stats",
+    "relaygr_kv_footprint_bytes_q8", "relaygr_kv_pool_bytes_for_q8", "relaygr_kv_pool_create_q8",
+    "relaygr_kv_pool_write", "relaygr_kv_pool_read", "relaygr_cache_attend",
     "relaygr_last_error",
 ]
 EXPANDER_STATS = ["hbm_hits", "dram_hits", "misses", "refusals", "spills", "dram_evictions", "dram_bytes", "dram_entries",
@@ -66,6 +68,11 @@ class BatchC(C.Structure):
                 ("prefix_emb", C.c_void_p), ("prefix_off", C.POINTER(C.c_int32)),
                 ("suffix_emb", C.c_void_p), ("suffix_off", C.POINTER(C.c_int32)),
                 ("cand_emb", C.c_void_p), ("cand_off", C.POINTER(C.c_int32))]
+
+
+class KvRowsC(C.Structure):
+    _fields_ = [("n_users", C.c_int32), ("handles", C.POINTER(C.c_uint64)), ("row_off", C.POINTER(C.c_int32)),
+                ("first_token", C.POINTER(C.c_int32)), ("key_len", C.POINTER(C.c_int32))]
 
 
 class AdmissionParamsC(C.Structure):
@@ -139,6 +146,12 @@ def load_library() -> C.CDLL:
         "relaygr_trigger_admit": (C.c_int, [vp, C.c_double, i32]),
         "relaygr_trigger_release": (C.c_int, [vp]),
         "relaygr_trigger_stats": (C.c_int, [vp, P(i64), P(i64), P(i64), P(i64)]),
+        "relaygr_kv_footprint_bytes_q8": (sz, [P(ModelConfigC), i32]),
+        "relaygr_kv_pool_bytes_for_q8": (sz, [P(ModelConfigC), i32, i32]),
+        "relaygr_kv_pool_create_q8": (C.c_int, [P(ModelConfigC), vp, sz, i32, P(vp)]),
+        "relaygr_kv_pool_write": (C.c_int, [vp, i32, P(KvRowsC), vp, i64, vp, i64, vp]),
+        "relaygr_kv_pool_read": (C.c_int, [vp, i32, P(KvRowsC), vp, i64, vp, i64, vp]),
+        "relaygr_cache_attend": (C.c_int, [vp, vp, i32, P(KvRowsC), i32, vp, i64, vp, i64, vp]),
         "relaygr_last_error": (C.c_char_p, []),
     }
     for name, (res, args) in sig.items():
@@ -268,21 +281,24 @@ def relaygr_ctx_profile_read(ctx: Context, kernel_class: str):
 
 
 class KvPool:
-    """relaygr_kv_pool over a torch-allocated device slab."""
+    """relaygr_kv_pool over a torch-allocated device slab; quantized: K and V in 8 bits (relaygr_kv_pool_create_q8)."""
 
-    def __init__(self, cfg: ModelConfigC, dtype: str, slab_bytes: int, page_tokens: int = 256, device: str = "cuda:0"):
+    def __init__(self, cfg: ModelConfigC, dtype: str, slab_bytes: int, page_tokens: int = 256, device: str = "cuda:0",
+                 quantized: bool = False):
         lib = load_library()
         self.cfg = cfg
         self.dtype = dtype
+        self.quantized = quantized
         self.device = torch.device(device)
         self.slab = torch.empty(slab_bytes, dtype=torch.uint8, device=self.device)
         h = C.c_void_p()
-        _check(lib.relaygr_kv_pool_create(C.byref(cfg), self.slab.data_ptr(), slab_bytes, page_tokens, C.byref(h)))
+        create = lib.relaygr_kv_pool_create_q8 if quantized else lib.relaygr_kv_pool_create
+        _check(create(C.byref(cfg), self.slab.data_ptr(), slab_bytes, page_tokens, C.byref(h)))
         self.handle = h
 
     def elements(self) -> torch.Tensor:
-        """The slab viewed in the storage dtype (for inspection with relaygr_kv_pool_locate)."""
-        return self.slab.view(_torch_dtype(self.dtype))
+        """The slab viewed in the storage dtype, or as its 8-bit codes (for inspection with relaygr_kv_pool_locate)."""
+        return self.slab.view(torch.float8_e4m3fn if self.quantized else _torch_dtype(self.dtype))
 
     def close(self):
         if getattr(self, "handle", None):
@@ -332,6 +348,105 @@ def relaygr_kv_pool_locate(pool: KvPool, handle: int, layer: int, token: int, fe
     k, v = C.c_int64(), C.c_int64()
     _check(load_library().relaygr_kv_pool_locate(pool.handle, handle, layer, token, feature, C.byref(k), C.byref(v)))
     return k.value, v.value
+
+
+# ---- 8-bit pools -----------------------------------------------------------------------------
+def relaygr_kv_footprint_bytes_q8(cfg: ModelConfigC, prefix_len: int) -> int:
+    return load_library().relaygr_kv_footprint_bytes_q8(C.byref(cfg), prefix_len)
+
+
+def relaygr_kv_pool_bytes_for_q8(cfg: ModelConfigC, prefix_len: int, page_tokens: int) -> int:
+    return load_library().relaygr_kv_pool_bytes_for_q8(C.byref(cfg), prefix_len, page_tokens)
+
+
+class KvRows:
+    """The host arrays of a relaygr_kv_rows: which rows of a call's tensors belong to which entry, and where in it they are.
+
+    row_off: n_users + 1 offsets.  first_token (write, read): token of the entry that a user's first row is; None: 0.  key_len
+    (attend): tokens of the entry that take part; None: all.  Made once, used in any number of calls."""
+
+    def __init__(self, handles: Sequence[int], row_off: Sequence[int], first_token: Optional[Sequence[int]] = None,
+                 key_len: Optional[Sequence[int]] = None):
+        self.handles = np.array(handles, dtype=np.uint64)
+        self.row_off = np.array(row_off, dtype=np.int32)
+        self.first_token = None if first_token is None else np.array(first_token, dtype=np.int32)
+        self.key_len = None if key_len is None else np.array(key_len, dtype=np.int32)
+        self.n_users = self.handles.size
+        for name, a, n in (("handles", self.handles, self.n_users), ("row_off", self.row_off, self.n_users + 1),
+                           ("first_token", self.first_token, self.n_users), ("key_len", self.key_len, self.n_users)):
+            if a is not None and a.shape != (n,):
+                raise RelayGRError(RELAYGR_EINVAL, f"KvRows: {name} has shape {a.shape}, ({n},) is needed")
+        self.n_rows = int(self.row_off[-1])
+
+        def ptr(a):
+            return None if a is None else a.ctypes.data_as(C.POINTER(C.c_int32))
+        self.c = KvRowsC(self.n_users, self.handles.ctypes.data_as(C.POINTER(C.c_uint64)), ptr(self.row_off), ptr(self.first_token),
+                         ptr(self.key_len))
+
+
+def _kv_rows_array(what: str, pool: KvPool, rows: KvRows, t: torch.Tensor):
+    """(address, elements between rows) of a tensor [rows, d_model] or [rows, heads, d_head] on the pool's device."""
+    d, heads = pool.cfg.d_model, pool.cfg.n_heads
+    ok = t.dtype == _torch_dtype(pool.dtype) and t.device == pool.slab.device and t.shape[0] == rows.n_rows
+    if t.dim() == 2:
+        ok = ok and t.shape[1] == d and t.stride(1) == 1
+    else:
+        ok = ok and t.dim() == 3 and t.shape[1:] == (heads, d // heads) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == d // heads)
+    if not ok:
+        raise RelayGRError(RELAYGR_EINVAL, f"{what}: needs {rows.n_rows} rows of {d} adjacent {pool.dtype} elements on {pool.slab.device}, got "
+                                           f"{tuple(t.shape)} of {t.dtype} on {t.device} with strides {t.stride()}")
+    # (the stride of a single row means nothing: torch may report any)
+    return (t.data_ptr() if rows.n_rows else None), (t.stride(0) if rows.n_rows > 1 else d)
+
+
+def _on_stream(pool: KvPool, stream):
+    """The stream of a call (default: the current one of the pool's device), as a torch stream and as a raw handle."""
+    if stream is None:
+        s = torch.cuda.current_stream(pool.slab.device)
+        return s, s.cuda_stream
+    if isinstance(stream, int):
+        return torch.cuda.ExternalStream(stream, device=pool.slab.device), stream
+    return stream, stream.cuda_stream
+
+
+def _new_rows(pool: KvPool, rows: KvRows, stream) -> torch.Tensor:
+    """A result's memory, taken on the stream that writes it."""
+    with torch.cuda.stream(stream):
+        return torch.empty((rows.n_rows, pool.cfg.d_model), dtype=_torch_dtype(pool.dtype), device=pool.slab.device)
+
+
+def relaygr_kv_pool_write(pool: KvPool, layer: int, rows: KvRows, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+    """Quantises rows of K and V ([rows, d_model] or [rows, heads, d_head]) into the entries' tokens first_token on."""
+    kp, ks = _kv_rows_array("kv_pool_write: k", pool, rows, k)
+    vp, vs = _kv_rows_array("kv_pool_write: v", pool, rows, v)
+    _, st = _on_stream(pool, stream)
+    with torch.cuda.device(pool.slab.device):
+        _check(load_library().relaygr_kv_pool_write(pool.handle, layer, C.byref(rows.c), kp, ks, vp, vs, st))
+
+
+def relaygr_kv_pool_read(pool: KvPool, layer: int, rows: KvRows, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+                         stream=None):
+    """(k, v): the values that tokens of the entries stand for, [rows, d_model] each (made here if not given)."""
+    ts, st = _on_stream(pool, stream)
+    k = _new_rows(pool, rows, ts) if k is None else k
+    v = _new_rows(pool, rows, ts) if v is None else v
+    kp, ks = _kv_rows_array("kv_pool_read: k", pool, rows, k)
+    vp, vs = _kv_rows_array("kv_pool_read: v", pool, rows, v)
+    with torch.cuda.device(pool.slab.device):
+        _check(load_library().relaygr_kv_pool_read(pool.handle, layer, C.byref(rows.c), kp, ks, vp, vs, st))
+    return k, v
+
+
+def relaygr_cache_attend(ctx: Context, pool: KvPool, layer: int, rows: KvRows, q: torch.Tensor, causal: bool = False,
+                         out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """One layer's attention of query rows over entries of an 8-bit pool, in the context's form: [rows, d_model] (made here if not given)."""
+    ts, st = _on_stream(pool, stream)
+    out = _new_rows(pool, rows, ts) if out is None else out
+    qp, qs = _kv_rows_array("cache_attend: q", pool, rows, q)
+    op, os_ = _kv_rows_array("cache_attend: out", pool, rows, out)
+    with torch.cuda.device(pool.slab.device):
+        _check(load_library().relaygr_cache_attend(ctx.handle, pool.handle, layer, C.byref(rows.c), int(causal), qp, qs, op, os_, st))
+    return out
 
 
 # ---- DRAM tier -------------------------------------------------------------------------------

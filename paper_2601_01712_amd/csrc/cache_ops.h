@@ -1,0 +1,26 @@
+// The host side of the 8-bit cache's calls: entry points of cache_ops.hip, and what engine.hip needs of them.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "../../include/relaygr.h"
+#include "kv_pool.h"
+
+namespace relaygr {
+
+// One relaygr_cache_attend on a stream: `scratch` holds the partial sums of rows that are cut along the keys (null: none are cut).
+struct AttendCall {
+  const relaygr_kv_rows* rows;
+  int32_t layer, causal;
+  const void* q;
+  int64_t q_stride;
+  void* out;
+  int64_t out_stride;
+  bool softmax;
+  int n_cus;
+  char* scratch;
+  size_t scratch_bytes;
+};
+int attend8(KvPool* pool, const AttendCall& call, hipStream_t st);
+
+}  // namespace relaygr

@@ -1,0 +1,231 @@
+// C-ABI entry points of the 8-bit K/V cache (kv8.h, attend8.h): writing rows, reading them back, and the planning and launches of
+// attention over them, whose entry point is engine.hip's (it takes a context's scratch).
+#include "cache_ops.h"
+
+#include <algorithm>
+#include <cmath>
+#include <vector>
+
+#include "attend8.h"
+#include "errors.h"
+#include "kv8.h"
+
+using namespace relaygr;
+
+#define LAUNCH_CHECK(name)                                                                     \
+  do {                                                                                         \
+    hipError_t e_ = hipGetLastError();                                                         \
+    if (e_ != hipSuccess) return fail(RELAYGR_EHIP, "launch %s: %s", name, hipGetErrorString(e_)); \
+  } while (0)
+
+namespace {
+
+// Rows of a [rows, d] array must be 16-byte aligned runs of d elements.
+int check_rows_array(const char* what, const char* name, const void* base, int64_t stride, int d) {
+  if (!base) return fail(RELAYGR_EINVAL, "%s: %s is null", what, name);
+  if (((uintptr_t)base & 15) || stride % 8) return fail(RELAYGR_EINVAL, "%s: rows of %s are not 16-byte aligned", what, name);
+  if (stride < d) return fail(RELAYGR_EINVAL, "%s: %s has a row stride of %lld elements, below d_model", what, name, (long long)stride);
+  return RELAYGR_OK;
+}
+
+// The batch's entries, after the checks that all three calls share.
+int resolve_rows(const char* what, KvPool* pool, int32_t layer, const relaygr_kv_rows* r, std::vector<PoolEntry>* entries) {
+  if (!pool || !r) return fail(RELAYGR_EINVAL, "%s: null argument", what);
+  if (!pool->q8) return fail(RELAYGR_EINVAL, "%s: the pool does not hold 8-bit K/V", what);
+  if (layer < 0 || layer >= pool->cfg.n_layers) return fail(RELAYGR_EINVAL, "%s: layer %d out of range", what, layer);
+  if (r->n_users < 0) return fail(RELAYGR_EINVAL, "%s: n_users < 0", what);
+  if (r->n_users == 0) return RELAYGR_OK;
+  if (!r->handles || !r->row_off) return fail(RELAYGR_EINVAL, "%s: null handles or row offsets", what);
+  if (r->row_off[0] != 0) return fail(RELAYGR_EINVAL, "%s: row offsets must start at 0", what);
+  for (int u = 0; u < r->n_users; ++u)
+    if (r->row_off[u + 1] < r->row_off[u]) return fail(RELAYGR_EINVAL, "%s: row offsets not monotone at user %d", what, u);
+  entries->resize(r->n_users);
+  for (int u = 0; u < r->n_users; ++u)
+    if (pool->resolve(r->handles[u], &(*entries)[u]) != RELAYGR_OK) return fail(RELAYGR_ENOENT, "%s: user %d: stale or unknown handle", what, u);
+  return RELAYGR_OK;
+}
+
+char* entry_tile0(const KvPool* pool, const PoolEntry& e) {
+  return (char*)pool->slab + (size_t)e.page0 * pool->page_bytes;
+}
+
+template <bool WRITE>
+int move_rows(const char* what, KvPool* pool, int32_t layer, const relaygr_kv_rows* r, void* k, int64_t k_stride, void* v, int64_t v_stride, hipStream_t st) {
+  std::vector<PoolEntry> entries;
+  int rc = resolve_rows(what, pool, layer, r, &entries);
+  if (rc != RELAYGR_OK || r->n_users == 0) return rc;
+  for (int u = 0; u < r->n_users; ++u) {
+    const int64_t first = r->first_token ? r->first_token[u] : 0, n = r->row_off[u + 1] - r->row_off[u];
+    if (first < 0 || first + n > entries[u].prefix_len)
+      return fail(RELAYGR_EINVAL, "%s: user %d: tokens %lld to %lld of an entry of %d", what, u, (long long)first, (long long)(first + n), entries[u].prefix_len);
+  }
+  if (r->row_off[r->n_users] == 0) return RELAYGR_OK;
+  const relaygr_model_config& cfg = pool->cfg;
+  if ((rc = check_rows_array(what, "k", k, k_stride, cfg.d_model)) != RELAYGR_OK) return rc;
+  if ((rc = check_rows_array(what, "v", v, v_stride, cfg.d_model)) != RELAYGR_OK) return rc;
+  if (WRITE) {   // two users writing one entry would race
+    std::vector<relaygr_kv_handle> hs;
+    for (int u = 0; u < r->n_users; ++u) if (r->row_off[u + 1] > r->row_off[u]) hs.push_back(r->handles[u]);
+    std::sort(hs.begin(), hs.end());
+    if (std::adjacent_find(hs.begin(), hs.end()) != hs.end()) return fail(RELAYGR_EINVAL, "%s: two users of the batch carry the same handle", what);
+  }
+  (void)hipGetLastError();   // a failure the caller's own HIP calls left behind is not this call's
+  RowsParams p = {};
+  p.k = k; p.v = v; p.k_stride = k_stride; p.v_stride = v_stride;
+  p.tile_stride = pool->tile_stride;
+  p.codes_off = layer * pool->layer_stride;
+  p.scales_off = q8_scales_off(cfg, layer);
+  p.n_heads = cfg.n_heads;
+  const int dh = cfg.d_model / cfg.n_heads;
+  for (int u = 0; u < r->n_users;) {
+    p.n_users = 0; p.n_tiles = 0;
+    for (; u < r->n_users && p.n_users < kRowUsers; ++u) {
+      const int32_t first = r->first_token ? r->first_token[u] : 0, n = r->row_off[u + 1] - r->row_off[u];
+      if (n == 0) continue;
+      p.users[p.n_users++] = {entry_tile0(pool, entries[u]), first, n, r->row_off[u], p.n_tiles, 0};
+      p.n_tiles += (int)(((int64_t)first + n - 1) / kTile - first / kTile + 1);
+    }
+    if (p.n_users == 0) break;
+    const int64_t units = (int64_t)p.n_tiles * cfg.n_heads * 2;
+    const dim3 grid((unsigned)((units + 3) / 4));
+    auto launch = [&](auto h, auto dim) {
+      using H = decltype(h);
+      constexpr int DH = decltype(dim)::value;
+      if (WRITE) hipLaunchKernelGGL((kv8_write_kernel<H, DH>), grid, dim3(256), 0, st, p);
+      else hipLaunchKernelGGL((kv8_read_kernel<H, DH>), grid, dim3(256), 0, st, p);
+    };
+    auto by_dh = [&](auto h) {
+      switch (dh) {
+        case 32: launch(h, std::integral_constant<int, 32>()); break;
+        case 64: launch(h, std::integral_constant<int, 64>()); break;
+        default: launch(h, std::integral_constant<int, 128>()); break;
+      }
+    };
+    if (cfg.dtype == RELAYGR_DTYPE_FP16) by_dh(F16());
+    else by_dh(Bf16());
+    LAUNCH_CHECK(what);
+  }
+  return RELAYGR_OK;
+}
+
+template <typename H, bool SM>
+void launch_attend(const AttendParams& p, int dh, bool wide, int rows, int row_base, bool cut, hipStream_t st) {
+  const int nh = p.n_heads;
+  const dim3 grid(nh >= 8 ? p.n_items * nh : (p.n_items + 8 / nh - 1) / (8 / nh) * 8), block(kAttendWaves * 64);
+  switch (dh) {
+    case 32:
+      if (wide) hipLaunchKernelGGL((attend8_kernel<H, 32, 2, SM>), grid, block, 0, st, p);
+      else hipLaunchKernelGGL((attend8_kernel<H, 32, 1, SM>), grid, block, 0, st, p);
+      break;
+    case 64:
+      if (wide) hipLaunchKernelGGL((attend8_kernel<H, 64, 2, SM>), grid, block, 0, st, p);
+      else hipLaunchKernelGGL((attend8_kernel<H, 64, 1, SM>), grid, block, 0, st, p);
+      break;
+    default: hipLaunchKernelGGL((attend8_kernel<H, 128, 1, SM>), grid, block, 0, st, p); break;
+  }
+  if (cut) hipLaunchKernelGGL((attend8_join_kernel<H, SM>), dim3((unsigned)(((int64_t)rows * (p.d / 4) + 255) / 256)), dim3(256), 0, st, p, rows, row_base);
+}
+
+}  // namespace
+
+int relaygr::attend8(KvPool* pool, const AttendCall& c, hipStream_t st) {
+  static const char* what = "cache_attend";
+  std::vector<PoolEntry> entries;
+  const relaygr_kv_rows* r = c.rows;
+  int rc = resolve_rows(what, pool, c.layer, r, &entries);
+  if (rc != RELAYGR_OK || r->n_users == 0) return rc;
+  const relaygr_model_config& cfg = pool->cfg;
+  const int d = cfg.d_model, H = cfg.n_heads, dh = d / H;
+  struct Work { int user, rows, keys; };
+  std::vector<Work> work;
+  int64_t rows_all = 0;
+  int most_rows = 0;
+  for (int u = 0; u < r->n_users; ++u) {
+    const int keys = r->key_len ? r->key_len[u] : entries[u].prefix_len, n = r->row_off[u + 1] - r->row_off[u];
+    if (keys < 0 || keys > entries[u].prefix_len) return fail(RELAYGR_EINVAL, "%s: user %d: %d keys of an entry of %d tokens", what, u, keys, entries[u].prefix_len);
+    if (n == 0) continue;
+    work.push_back({u, n, keys});
+    rows_all += n;
+    most_rows = std::max(most_rows, n);
+  }
+  if (work.empty()) return RELAYGR_OK;
+  if ((rc = check_rows_array(what, "q", c.q, c.q_stride, d)) != RELAYGR_OK) return rc;
+  if ((rc = check_rows_array(what, "out", c.out, c.out_stride, d)) != RELAYGR_OK) return rc;
+
+  const bool wide = dh <= 64 && most_rows > 32;
+  const int item_rows = wide ? 64 : 32;
+  // pieces of the key sequences
+  const int64_t slots = 2 * c.n_cus;
+  int64_t items = 0, tiles = 0;
+  for (const Work& w : work) {
+    const int64_t rt = (w.rows + item_rows - 1) / item_rows;
+    items += rt * H;
+    tiles += rt * H * ((w.keys + kTile - 1) / kTile);
+  }
+  int64_t per = std::max<int64_t>(kAttendWaves, (tiles + slots - 1) / slots);
+  if (items >= 2 * slots || !c.scratch) per = 1 << 30;
+  const size_t row_bytes = (size_t)d * 4 + (c.softmax ? (size_t)H * 8 : 0);
+  auto parts_of = [&](const Work& w) { const int64_t nk = (w.keys + kTile - 1) / kTile; return (int)std::max<int64_t>(1, (nk + per - 1) / per); };
+  int64_t partial_rows;
+  for (;; per *= 2) {
+    partial_rows = 0;
+    for (const Work& w : work) { const int parts = parts_of(w); if (parts > 1) partial_rows += (int64_t)parts * w.rows; }
+    if (partial_rows == 0 || ((size_t)partial_rows * row_bytes <= c.scratch_bytes && partial_rows < (1ll << 31))) break;
+  }
+
+  (void)hipGetLastError();
+  AttendParams p = {};
+  p.q = (const uint16_t*)c.q; p.out = (uint16_t*)c.out; p.q_stride = c.q_stride; p.out_stride = c.out_stride;
+  p.tile_stride = pool->tile_stride;
+  p.scales_off = q8_scales_off(cfg, c.layer) - c.layer * pool->layer_stride;
+  p.part = (float*)c.scratch;
+  p.ml = (float*)(c.scratch + (size_t)partial_rows * d * 4);
+  p.d = d; p.n_heads = H; p.causal = c.causal ? 1 : 0;
+  p.score_mul = 1.4426950408889634f / sqrtf((float)dh);
+  int32_t part0 = 0;
+  for (size_t i = 0; i < work.size();) {
+    p.n_users = 0; p.n_items = 0;
+    bool cut = false;
+    const int row_base = r->row_off[work[i].user];
+    int row_end = row_base;
+    for (; i < work.size() && p.n_users < kAttendUsers; ++i) {
+      const Work& w = work[i];
+      const int parts = parts_of(w), nk = (w.keys + kTile - 1) / kTile;
+      AttendUser& u = p.users[p.n_users++];
+      u.kv = entry_tile0(pool, entries[w.user]) + c.layer * pool->layer_stride;
+      u.row0 = r->row_off[w.user]; u.rows = w.rows; u.keys = w.keys;
+      u.item0 = p.n_items; u.part0 = part0; u.parts = parts; u.per = std::max(1, (nk + parts - 1) / parts); u.pad_ = 0;
+      p.n_items += (w.rows + item_rows - 1) / item_rows * parts;
+      if (parts > 1) { part0 += parts * w.rows; cut = true; }
+      row_end = u.row0 + w.rows;
+    }
+    auto go = [&](auto h) {
+      using HT = decltype(h);
+      if (c.softmax) launch_attend<HT, true>(p, dh, wide, row_end - row_base, row_base, cut, st);
+      else launch_attend<HT, false>(p, dh, wide, row_end - row_base, row_base, cut, st);
+    };
+    if (cfg.dtype == RELAYGR_DTYPE_FP16) go(F16());
+    else go(Bf16());
+    LAUNCH_CHECK(what);
+  }
+  return RELAYGR_OK;
+}
+
+// (the planning allocates host memory: running out of it is an error code of the call)
+#define NO_THROW(expr)                                                                          \
+  try {                                                                                         \
+    return expr;                                                                                \
+  } catch (...) {                                                                               \
+    return fail(RELAYGR_EINVAL, "out of host memory");                                          \
+  }
+
+extern "C" int relaygr_kv_pool_write(relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, const void* k, int64_t k_stride,
+                                     const void* v, int64_t v_stride, void* hip_stream) {
+  NO_THROW(move_rows<true>("kv_pool_write", reinterpret_cast<KvPool*>(pool), layer, rows, const_cast<void*>(k), k_stride, const_cast<void*>(v), v_stride,
+                           (hipStream_t)hip_stream))
+}
+
+extern "C" int relaygr_kv_pool_read(relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, void* k, int64_t k_stride, void* v,
+                                    int64_t v_stride, void* hip_stream) {
+  NO_THROW(move_rows<false>("kv_pool_read", reinterpret_cast<KvPool*>(pool), layer, rows, k, k_stride, v, v_stride, (hipStream_t)hip_stream))
+}

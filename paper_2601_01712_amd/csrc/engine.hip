@@ -16,11 +16,13 @@
 
 #include "../../include/relaygr.h"
 #include "attention.h"
+#include "cache_ops.h"
 #include "common.h"
 #include "errors.h"
 #include "fp32.h"
 #include "gemm.h"
 #include "gemm_bf16.h"
+#include "kv8.h"
 #include "kv_pool.h"
 #include "rowwise.h"
 #include "staging.h"
@@ -81,6 +83,21 @@ extern "C" size_t relaygr_kv_pool_bytes_for(const relaygr_model_config* cfg, int
   if (!config_ok(cfg) || prefix_len < 0 || page_tokens < kTile || page_tokens % kTile) return 0;
   size_t pages = ((size_t)prefix_len + page_tokens - 1) / page_tokens;
   return pages * (size_t)2 * cfg->n_layers * page_tokens * cfg->d_model * elem_bytes(*cfg);
+}
+
+// 8-bit pools serve the 16-bit storage types: fp32 arithmetic behind codes of four significant bits has nothing to gain.
+static bool q8_config_ok(const relaygr_model_config* c) { return config_ok(c) && is_half16(*c); }
+
+extern "C" size_t relaygr_kv_footprint_bytes_q8(const relaygr_model_config* cfg, int32_t prefix_len) {
+  if (!q8_config_ok(cfg) || prefix_len < 0) return 0;
+  const size_t blocks = ((size_t)prefix_len + kTile - 1) / kTile * cfg->n_layers * cfg->n_heads * 2;
+  return (size_t)2 * cfg->n_layers * (size_t)prefix_len * cfg->d_model + blocks * sizeof(float);
+}
+
+extern "C" size_t relaygr_kv_pool_bytes_for_q8(const relaygr_model_config* cfg, int32_t prefix_len, int32_t page_tokens) {
+  if (!q8_config_ok(cfg) || prefix_len < 0 || page_tokens < kTile || page_tokens % kTile) return 0;
+  const size_t pages = ((size_t)prefix_len + page_tokens - 1) / page_tokens;
+  return pages * (page_tokens / kTile) * (size_t)q8_tile_bytes(*cfg);
 }
 
 // ---- per-call plan ----------------------------------------------------------------------------
@@ -464,14 +481,14 @@ extern "C" int relaygr_ctx_profile_read(relaygr_ctx* c, int32_t cls, double* tot
 }
 
 // ---- pool ABI ---------------------------------------------------------------------------------
-extern "C" int relaygr_kv_pool_create(const relaygr_model_config* cfg, void* slab_dev, size_t slab_bytes,
-                                      int32_t page_tokens, relaygr_kv_pool** out) {
+static int pool_create(const relaygr_model_config* cfg, void* slab_dev, size_t slab_bytes, int32_t page_tokens, bool q8, relaygr_kv_pool** out) {
   if (!out) return fail(RELAYGR_EINVAL, "kv_pool_create: out is null");
   *out = nullptr;
   if (!config_ok(cfg)) return fail(RELAYGR_EINVAL, "kv_pool_create: unsupported model config");
+  if (q8 && !q8_config_ok(cfg)) return fail(RELAYGR_EINVAL, "kv_pool_create_q8: 8-bit K/V are for the 16-bit storage types");
   if (!slab_dev || ((uintptr_t)slab_dev & 255)) return fail(RELAYGR_EINVAL, "kv_pool_create: slab null or not 256-byte aligned");
   if (page_tokens < kTile || page_tokens % kTile) return fail(RELAYGR_EINVAL, "kv_pool_create: page_tokens must be a positive multiple of 64");
-  size_t page_bytes = (size_t)2 * cfg->n_layers * page_tokens * cfg->d_model * elem_bytes(*cfg);
+  const size_t page_bytes = q8 ? relaygr_kv_pool_bytes_for_q8(cfg, page_tokens, page_tokens) : relaygr_kv_pool_bytes_for(cfg, page_tokens, page_tokens);
   int64_t n_pages = (int64_t)(slab_bytes / page_bytes);
   if (n_pages < 1) return fail(RELAYGR_ENOSPC, "kv_pool_create: slab smaller than one page (%zu bytes)", page_bytes);
   if (n_pages * (int64_t)page_tokens >= (1ll << 31)) return fail(RELAYGR_EINVAL, "kv_pool_create: slab holds 2^31 tokens or more");
@@ -482,11 +499,23 @@ extern "C" int relaygr_kv_pool_create(const relaygr_model_config* cfg, void* sla
   p->slab_bytes = slab_bytes;
   p->page_tokens = page_tokens;
   p->n_pages = n_pages;
+  p->q8 = q8;
+  p->page_bytes = page_bytes;
   p->layer_stride = (int64_t)2 * kTile * cfg->d_model;
-  p->tile_stride = p->layer_stride * cfg->n_layers;
+  p->tile_stride = q8 ? q8_tile_bytes(*cfg) : p->layer_stride * cfg->n_layers;
   p->free_extents[0] = n_pages;
   *out = reinterpret_cast<relaygr_kv_pool*>(p);
   return RELAYGR_OK;
+}
+
+extern "C" int relaygr_kv_pool_create(const relaygr_model_config* cfg, void* slab_dev, size_t slab_bytes,
+                                      int32_t page_tokens, relaygr_kv_pool** out) {
+  return pool_create(cfg, slab_dev, slab_bytes, page_tokens, false, out);
+}
+
+extern "C" int relaygr_kv_pool_create_q8(const relaygr_model_config* cfg, void* slab_dev, size_t slab_bytes,
+                                         int32_t page_tokens, relaygr_kv_pool** out) {
+  return pool_create(cfg, slab_dev, slab_bytes, page_tokens, true, out);
 }
 
 extern "C" void relaygr_kv_pool_destroy(relaygr_kv_pool* pool) { delete reinterpret_cast<KvPool*>(pool); }
@@ -542,7 +571,10 @@ extern "C" int relaygr_kv_pool_locate(relaygr_kv_pool* pool, relaygr_kv_handle h
   int64_t tile = e.page0 * (p->page_tokens / kTile) + token / kTile;
   int r = token % kTile;
   int64_t base = tile * p->tile_stride + (int64_t)layer * p->layer_stride + (int64_t)head * 2 * kTile * dh;
-  if (p->cfg.dtype == RELAYGR_DTYPE_FP32) {
+  if (p->q8) {
+    *k_index = base + KvLayout8::k_off(r, f, dh);
+    *v_index = base + KvLayout8::v_off(r, f, dh);
+  } else if (p->cfg.dtype == RELAYGR_DTYPE_FP32) {
     *k_index = base + KvLayout<float>::k_off(r, f, dh);
     *v_index = base + KvLayout<float>::v_off(r, f, dh);
   } else {
@@ -1036,6 +1068,7 @@ static int run(relaygr_ctx* c, relaygr_kv_pool* pool, const relaygr_batch* b, Mo
     const relaygr_model_config &a = kp->cfg, &m = c->cfg;
     if (a.n_layers != m.n_layers || a.d_model != m.d_model || a.n_heads != m.n_heads || a.dtype != m.dtype)
       return fail(RELAYGR_EINVAL, "pool and context were created for different model shapes");
+    if (kp->q8) return fail(RELAYGR_EINVAL, "the pool holds 8-bit K/V");
   }
   hipStream_t st = (hipStream_t)stream;
   (void)hipGetLastError();   // a failure the caller's own HIP calls left behind is not this call's: launch checks below start clean
@@ -1049,6 +1082,25 @@ static int run(relaygr_ctx* c, relaygr_kv_pool* pool, const relaygr_batch* b, Mo
   if (c->cfg.dtype == RELAYGR_DTYPE_FP32) rc = run_typed<float>(c, kp, b, mode, scores, cs, st, capturing);
   else if (c->cfg.dtype == RELAYGR_DTYPE_FP16) rc = run_typed<__half>(c, kp, b, mode, scores, cs, st, capturing);
   else rc = run_typed<__hip_bfloat16>(c, kp, b, mode, scores, cs, st, capturing);
+  if (!capturing) { c->last_stream = st; c->has_call = true; }
+  return rc;
+}
+
+extern "C" int relaygr_cache_attend(relaygr_ctx* c, relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, int32_t causal, const void* q,
+                                    int64_t q_stride, void* out, int64_t out_stride, void* hip_stream) {
+  if (!c || !pool) return fail(RELAYGR_EINVAL, "cache_attend: null argument");
+  KvPool* kp = reinterpret_cast<KvPool*>(pool);
+  const relaygr_model_config &a = kp->cfg, &m = c->cfg;
+  if (a.n_layers != m.n_layers || a.d_model != m.d_model || a.n_heads != m.n_heads || a.dtype != m.dtype)
+    return fail(RELAYGR_EINVAL, "cache_attend: pool and context were created for different model shapes");
+  std::lock_guard<std::mutex> call_lock(c->mu);
+  hipStream_t st = (hipStream_t)hip_stream;
+  const size_t wp = wpack_bytes(c->cfg);
+  const AttendCall call = {rows, layer, causal, q, q_stride, out, out_stride, c->attn_form == RELAYGR_ATTN_SOFTMAX, c->n_cus, c->scratch + wp, c->scratch_bytes - wp};
+  const bool capturing = stream_is_capturing(st);      // (as in run)
+  if (!capturing && c->has_call && c->last_stream != st) HIP_TRY(order_behind(st, c->last_stream, c->call_done));
+  int rc;
+  try { rc = attend8(kp, call, st); } catch (...) { rc = fail(RELAYGR_EINVAL, "cache_attend: out of host memory"); }
   if (!capturing) { c->last_stream = st; c->has_call = true; }
   return rc;
 }

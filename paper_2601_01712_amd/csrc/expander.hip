@@ -25,9 +25,7 @@ using namespace relaygr;
     if (e_ != hipSuccess) return fail(RELAYGR_EHIP, "%s: %s", #expr, hipGetErrorString(e_));   \
   } while (0)
 
-static size_t page_bytes(const KvPool* p) {
-  return (size_t)2 * p->cfg.n_layers * p->page_tokens * p->cfg.d_model * elem_bytes(p->cfg);
-}
+static size_t page_bytes(const KvPool* p) { return p->page_bytes; }
 static char* extent_ptr(const KvPool* p, const PoolEntry& e) { return (char*)p->slab + (size_t)e.page0 * page_bytes(p); }
 
 extern "C" size_t relaygr_kv_pool_entry_bytes(relaygr_kv_pool* pool, relaygr_kv_handle h) {
@@ -229,6 +227,8 @@ extern "C" int relaygr_expander_create(relaygr_kv_pool* pool, size_t dram_budget
   ex->dram.cfg = ex->hbm->cfg;
   ex->dram.slab = ex->arena;
   ex->dram.slab_bytes = (size_t)pages * pb;
+  ex->dram.q8 = ex->hbm->q8;
+  ex->dram.page_bytes = pb;
   ex->dram.page_tokens = ex->hbm->page_tokens;
   ex->dram.n_pages = pages;
   ex->dram.layer_stride = ex->hbm->layer_stride;

@@ -32,8 +32,10 @@ struct KvPool {
   size_t slab_bytes = 0;
   int32_t page_tokens = 0;
   int64_t n_pages = 0;
-  int64_t tile_stride = 0;    // elements per 64-token tile block (all layers)
-  int64_t layer_stride = 0;   // elements per layer inside a tile block
+  bool q8 = false;            // K and V in 8 bits (layout in kv8.h)
+  size_t page_bytes = 0;
+  int64_t tile_stride = 0;    // elements (8 bits: bytes) per 64-token tile block (all layers)
+  int64_t layer_stride = 0;   // elements (8 bits: bytes) per layer inside a tile block
   std::mutex mu;
   std::map<int64_t, int64_t> free_extents;   // first page -> page count
   std::vector<PoolEntry> entries;
@@ -50,5 +52,11 @@ struct KvPool {
 };
 
 inline int elem_bytes(const relaygr_model_config& c) { return c.dtype == RELAYGR_DTYPE_FP32 ? 4 : 2; }
+
+// 8-bit pools: bytes of a tile block, the codes of all layers and then the scales, and where a layer's scales start in it.
+inline int64_t q8_scales_off(const relaygr_model_config& c, int layer) {
+  return (int64_t)c.n_layers * 2 * RELAYGR_TILE_TOKENS * c.d_model + (int64_t)layer * c.n_heads * 8;
+}
+inline int64_t q8_tile_bytes(const relaygr_model_config& c) { return (q8_scales_off(c, c.n_layers) + 127) / 128 * 128; }
 
 }  // namespace relaygr
