@@ -215,7 +215,9 @@ size_t relaygr_kv_footprint_bytes_q8(const relaygr_model_config* cfg, int32_t pr
 size_t relaygr_kv_pool_bytes_for_q8(const relaygr_model_config* cfg, int32_t prefix_len, int32_t page_tokens);
 /* relaygr_kv_pool_create for K and V in 8 bits.  A page holds page_tokens / 64 tiles of every layer's codes and scales
  * (relaygr_kv_pool_bytes_for_q8).  Every relaygr_kv_pool_* and relaygr_expander_* call takes such a pool (relaygr_kv_pool_locate then counts in
- * bytes, and says where codes are), and so do the three calls below. */
+ * bytes, and says where codes are); so do the three calls below, relaygr_prefill_prefix, which quantises each layer's K and V as it has computed
+ * them (its own attention reads them as computed), and the relaygr_rank_* calls, whose scores are exactly those of a 16-bit pool that
+ * holds the values the codes stand for. */
 int  relaygr_kv_pool_create_q8(const relaygr_model_config* cfg, void* slab_dev, size_t slab_bytes,
                                int32_t page_tokens, relaygr_kv_pool** out);
 

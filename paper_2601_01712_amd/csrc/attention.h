@@ -20,6 +20,7 @@
 
 #include "common.h"
 #include "gemm.h"
+#include "kv8.h"
 
 namespace relaygr {
 
@@ -44,6 +45,7 @@ struct AttnParams {
   int n_rows;
   int gs;             // key splits taken inside one workgroup and added in LDS: 16-bit 1 or 2 (wavefront groups), fp32 1 or 8 (wavefronts)
   int shared_tiles;   // 16-bit, gs = 2: key tiles from which on a piece is shared between the groups (attn_shared_tiles)
+  int64_t scales_off; // 8-bit pool: bytes from a tile's codes of this layer to the layer's scales (kv8.h)
 };
 
 // ---- bf16 MFMA kernel ---------------------------------------------------------------------------
@@ -217,7 +219,12 @@ __device__ __forceinline__ void softmax_track(const f32x16_t (&s)[NQ], const int
 // more workgroups than compute units, a piece takes half as long (attn_shared_tiles: the short pieces of such a launch are the first
 // group's alone, which sums them as a workgroup of one group does).  Both groups pass the same barriers; a group with fewer tiles pads
 // with empty ones.
-template <typename H, int DH, int NQ, int NW, bool SOFTMAX, int GS = 1>
+//
+// Q8: prefix tiles come from an 8-bit pool (kv8.h) where a user has an entry there; recomputed prefixes and suffixes are 16-bit tiles as ever.
+// A tile of codes passes through registers: each thread has its share of the next tile but one on its way while the workgroup works on a
+// tile, and turns it into the 16-bit tile's LDS image, which holds exactly what the codes stand for, when the ring slot becomes free.  Half the bytes of K/V
+// for 1/NW of a tile's conversions per wavefront (dh = 64, four wavefronts: 16 instructions and four LDS stores beside about 1800 cycles of SiLU).
+template <typename H, int DH, int NQ, int NW, bool SOFTMAX, int GS = 1, bool Q8 = false>
 __global__ __launch_bounds__(NW * GS * 64, (DH >= 128 || GS > 1) ? 1 : 512 / (NW * 64)) void attn_bf16_kernel(AttnParams p) {   // DH = 128: the 96 KiB tile ring admits one workgroup per compute unit
   constexpr int KS = DH / 16;              // k-steps of the first product
   constexpr int DB = DH / 32;              // 32-feature blocks of the output
@@ -372,6 +379,33 @@ __global__ __launch_bounds__(NW * GS * 64, (DH >= 128 || GS > 1) ? 1 : 512 / (NW
     }
   };
 
+  // 8-bit prefix tiles: a thread's chunks of the codes, and their way into the 16-bit image (chunk c: fragments 2c and 2c + 1)
+  constexpr int CH8 = Q8 ? TILE / 16 / (NW * 64) : 1;
+  static_assert(CH8 >= 1, "a tile of codes is at least one 16-byte chunk per thread");
+  const bool has8 = Q8 && at.kv_tile_stride != (int64_t)2 * kTile * p.d;      // (a tile of an 8-bit pool is never as small as one in single-layer scratch)
+  const char* kv8_base = reinterpret_cast<const char*>(at.kv) + (int64_t)p.layer * at.layer_stride(p.d) + (int64_t)head * TILE;
+  const int gtid = wave * 64 + lane;
+  uint4 raw[CH8];
+  float2 raw_scale = make_float2(1.f, 1.f);
+  auto fetch8 = [&](int tt, uint4 (&x)[CH8], float2& scale) {
+    if (!has8 || tt >= tr.nkp) return;
+    const char* tile = kv8_base + (int64_t)tt * at.kv_tile_stride;
+    scale = *reinterpret_cast<const float2*>(tile + p.scales_off - (int64_t)head * TILE + head * 8);
+#pragma unroll
+    for (int i = 0; i < CH8; ++i) x[i] = *reinterpret_cast<const uint4*>(tile + (i * (NW * 64) + gtid) * 16);
+  };
+  auto place8 = [&](int tt, int b, const uint4 (&x)[CH8], const float2& scale) {
+    if (!has8 || tt >= tr.nkp) { issue_tile(tt, b); return; }
+#pragma unroll
+    for (int i = 0; i < CH8; ++i) {
+      const int c = i * (NW * 64) + gtid;
+      const float sc = c < 4 * DH ? scale.x : scale.y;
+      uint16_t* dst = &bufs[b][(c >> 6) * 1024 + lane * 8];
+      *reinterpret_cast<u32x4_t*>(dst) = fp8_frag<H>(x[i].x, x[i].y, sc);
+      *reinterpret_cast<u32x4_t*>(dst + 512) = fp8_frag<H>(x[i].z, x[i].w, sc);
+    }
+  };
+
   // a wavefront whose rows all lie beyond the work item's last row only helps move tiles
   const bool wave_active = wave_s * 32 * NQ < at.nrows;
   const int nt = tr.t1 - tr.t0;
@@ -381,6 +415,17 @@ __global__ __launch_bounds__(NW * GS * 64, (DH >= 128 || GS > 1) ? 1 : 512 / (NW
   }
   if (nt == 0) start_from_own_key();
   if (nt > 0) {
+    if constexpr (Q8) {
+      uint4 raw1[CH8];
+      float2 scale1 = make_float2(1.f, 1.f);
+      fetch8(tr.t0, raw, raw_scale);
+      if (nt > 1) fetch8(tr.t0 + 1, raw1, scale1);
+      start_from_own_key();
+      place8(tr.t0, 0, raw, raw_scale);
+      if (nt > 1) place8(tr.t0 + 1, 1, raw1, scale1);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (16-bit tiles among them)
+      if (nt > 2) fetch8(tr.t0 + 2, raw, raw_scale);
+    } else {
     issue_tile(tr.t0, 0);
     if (nt > 1) issue_tile(tr.t0 + 1, 1);
     start_from_own_key();             // its loads are older than the tiles'
@@ -388,6 +433,7 @@ __global__ __launch_bounds__(NW * GS * 64, (DH >= 128 || GS > 1) ? 1 : 512 / (NW
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CHUNKS) : "memory");   // tile 0 landed, tile 1 may still fly
     } else {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
     }
     lds_barrier();
 
@@ -408,7 +454,12 @@ __global__ __launch_bounds__(NW * GS * 64, (DH >= 128 || GS > 1) ? 1 : 512 / (NW
     auto next_tile = [&](int i, int bn) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
-      if (i + 2 < nt) issue_tile(tr.t0 + i + 2, (bn == 2) ? 0 : bn + 1);
+      if constexpr (Q8) {
+        if (i + 2 < nt) place8(tr.t0 + i + 2, (bn == 2) ? 0 : bn + 1, raw, raw_scale);
+        if (i + 3 < nt) fetch8(tr.t0 + i + 3, raw, raw_scale);
+      } else if (i + 2 < nt) {
+        issue_tile(tr.t0 + i + 2, (bn == 2) ? 0 : bn + 1);
+      }
     };
 
     // one tile = two pipeline steps; MASKED tiles apply the per-element visibility test

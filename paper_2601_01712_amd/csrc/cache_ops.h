@@ -21,6 +21,9 @@ struct AttendCall {
   char* scratch;
   size_t scratch_bytes;
 };
+// A user's K and V of one layer, as 16-bit tiles in scratch, on their way into its 8-bit entry.
+struct TilesJob { int64_t page0; int32_t tiles; const void* src; };
+int quantise_tiles(const KvPool* pool, int layer, const TilesJob* jobs, int n_jobs, hipStream_t st);
 int attend8(KvPool* pool, const AttendCall& call, hipStream_t st);
 
 }  // namespace relaygr

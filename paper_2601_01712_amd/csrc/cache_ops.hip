@@ -128,6 +128,34 @@ void launch_attend(const AttendParams& p, int dh, bool wide, int rows, int row_b
 
 }  // namespace
 
+int relaygr::quantise_tiles(const KvPool* pool, int layer, const TilesJob* jobs, int n_jobs, hipStream_t st) {
+  const relaygr_model_config& cfg = pool->cfg;
+  const int d = cfg.d_model, dh = d / cfg.n_heads;
+  TilesParams p = {};
+  p.tile_stride = pool->tile_stride; p.src_stride = (int64_t)2 * kTile * d;
+  p.codes_off = layer * pool->layer_stride; p.scales_off = q8_scales_off(cfg, layer); p.n_heads = cfg.n_heads;
+  for (int j = 0; j < n_jobs;) {
+    p.n_users = 0; p.n_tiles = 0;
+    for (; j < n_jobs && p.n_users < kRowUsers; ++j) {
+      p.users[p.n_users++] = {(char*)pool->slab + (size_t)jobs[j].page0 * pool->page_bytes, (const uint16_t*)jobs[j].src, p.n_tiles, 0};
+      p.n_tiles += jobs[j].tiles;
+    }
+    const dim3 grid((unsigned)(((int64_t)p.n_tiles * cfg.n_heads * 2 + 3) / 4));
+    auto by_dh = [&](auto h) {
+      using H = decltype(h);
+      switch (dh) {
+        case 32: hipLaunchKernelGGL((kv8_tiles_kernel<H, 32>), grid, dim3(256), 0, st, p); break;
+        case 64: hipLaunchKernelGGL((kv8_tiles_kernel<H, 64>), grid, dim3(256), 0, st, p); break;
+        default: hipLaunchKernelGGL((kv8_tiles_kernel<H, 128>), grid, dim3(256), 0, st, p); break;
+      }
+    };
+    if (cfg.dtype == RELAYGR_DTYPE_FP16) by_dh(F16());
+    else by_dh(Bf16());
+    LAUNCH_CHECK("kv8_tiles");
+  }
+  return RELAYGR_OK;
+}
+
 int relaygr::attend8(KvPool* pool, const AttendCall& c, hipStream_t st) {
   static const char* what = "cache_attend";
   std::vector<PoolEntry> entries;

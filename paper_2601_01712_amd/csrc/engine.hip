@@ -620,17 +620,17 @@ int launch_attention<float>(const relaygr_model_config& cfg, const AttnParams& a
   return softmax ? launch_attention_f32<true>(cfg, ap, n_tiles, st) : launch_attention_f32<false>(cfg, ap, n_tiles, st);
 }
 
-template <typename H, bool SM>
+template <typename H, bool SM, bool Q8>
 static int launch_attention16(const relaygr_model_config& cfg, const AttnParams& ap, int n_tiles, int nq, hipStream_t st) {
   const int nh = cfg.n_heads;
   dim3 grid(nh >= 8 ? n_tiles * nh : (n_tiles + 8 / nh - 1) / (8 / nh) * 8);   // the kernel's order of heads and items
   switch (cfg.d_model / cfg.n_heads) {
-    case 32: hipLaunchKernelGGL((attn_bf16_kernel<H, 32, 1, 4, SM>), grid, dim3(256), 0, st, ap); break;
+    case 32: hipLaunchKernelGGL((attn_bf16_kernel<H, 32, 1, 4, SM, 1, Q8>), grid, dim3(256), 0, st, ap); break;
     case 64:
-      if (nq == 2 && ap.gs == 2) hipLaunchKernelGGL((attn_bf16_kernel<H, 64, 2, 4, SM, 2>), grid, dim3(512), 0, st, ap);
-      else if (ap.gs == 2) hipLaunchKernelGGL((attn_bf16_kernel<H, 64, 1, 4, SM, 2>), grid, dim3(512), 0, st, ap);
-      else if (nq == 2) hipLaunchKernelGGL((attn_bf16_kernel<H, 64, 2, 4, SM>), grid, dim3(256), 0, st, ap);
-      else hipLaunchKernelGGL((attn_bf16_kernel<H, 64, 1, 4, SM>), grid, dim3(256), 0, st, ap);
+      if (nq == 2 && ap.gs == 2) hipLaunchKernelGGL((attn_bf16_kernel<H, 64, 2, 4, SM, 2, Q8>), grid, dim3(512), 0, st, ap);
+      else if (ap.gs == 2) hipLaunchKernelGGL((attn_bf16_kernel<H, 64, 1, 4, SM, 2, Q8>), grid, dim3(512), 0, st, ap);
+      else if (nq == 2) hipLaunchKernelGGL((attn_bf16_kernel<H, 64, 2, 4, SM, 1, Q8>), grid, dim3(256), 0, st, ap);
+      else hipLaunchKernelGGL((attn_bf16_kernel<H, 64, 1, 4, SM, 1, Q8>), grid, dim3(256), 0, st, ap);
       break;
     case 128:
       // 256-row items: eight wavefronts of 32 rows.  With four of 64 rows a lane needs 458 registers, so that the scores come out of accumulation
@@ -638,21 +638,26 @@ static int launch_attention16(const relaygr_model_config& cfg, const AttnParams&
       // fragments are read from LDS twice as often, and the clock sinks with the load, so that less of it shows (us a call at d = 1024, 512 candidates
       // each, four / eight wavefronts: 16 users of 1000 keys 1381 / 1367, of 4096 2069 / 2058 and 2144 / 2159 on another card, of 8000 3070 / 3033; 24 of
       // 4000 3437 / 3351, of 12 000 6646 / 6679; 40 of 1000 3655 / 3569, of 2000 in the softmax form 4414 / 4285; full recompute of 12 000 keys 3962 / 3854).
-      if (nq == 2) hipLaunchKernelGGL((attn_bf16_kernel<H, 128, 1, 8, SM>), grid, dim3(512), 0, st, ap);
-      else hipLaunchKernelGGL((attn_bf16_kernel<H, 128, 1, 4, SM>), grid, dim3(256), 0, st, ap);
+      if (nq == 2) hipLaunchKernelGGL((attn_bf16_kernel<H, 128, 1, 8, SM, 1, Q8>), grid, dim3(512), 0, st, ap);
+      else hipLaunchKernelGGL((attn_bf16_kernel<H, 128, 1, 4, SM, 1, Q8>), grid, dim3(256), 0, st, ap);
       break;
     default: return fail(RELAYGR_EINVAL, "attention: unsupported d_head");
   }
   LAUNCH_CHECK("attn (16-bit)");
   return RELAYGR_OK;
 }
+template <typename H>
+static int launch_attention16_of(const relaygr_model_config& cfg, const AttnParams& ap, int n_tiles, int nq, bool softmax, hipStream_t st) {
+  if (ap.scales_off) return softmax ? launch_attention16<H, true, true>(cfg, ap, n_tiles, nq, st) : launch_attention16<H, false, true>(cfg, ap, n_tiles, nq, st);
+  return softmax ? launch_attention16<H, true, false>(cfg, ap, n_tiles, nq, st) : launch_attention16<H, false, false>(cfg, ap, n_tiles, nq, st);
+}
 template <>
 int launch_attention<__hip_bfloat16>(const relaygr_model_config& cfg, const AttnParams& ap, int n_tiles, int nq, bool softmax, hipStream_t st) {
-  return softmax ? launch_attention16<Bf16, true>(cfg, ap, n_tiles, nq, st) : launch_attention16<Bf16, false>(cfg, ap, n_tiles, nq, st);
+  return launch_attention16_of<Bf16>(cfg, ap, n_tiles, nq, softmax, st);
 }
 template <>
 int launch_attention<__half>(const relaygr_model_config& cfg, const AttnParams& ap, int n_tiles, int nq, bool softmax, hipStream_t st) {
-  return softmax ? launch_attention16<F16, true>(cfg, ap, n_tiles, nq, st) : launch_attention16<F16, false>(cfg, ap, n_tiles, nq, st);
+  return launch_attention16_of<F16>(cfg, ap, n_tiles, nq, softmax, st);
 }
 
 static int check_offsets(const int32_t* off, int n, const char* what) {
@@ -677,6 +682,9 @@ static int run_typed(relaygr_ctx* c, KvPool* pool, const relaygr_batch* b, Mode 
   Plan p;
   p.n_users = n;
   int64_t prow = 0, nrow = 0, sfx_tiles = 0, kvs_tiles = 0;
+  struct Quantise { int user; int64_t page0; };
+  std::vector<Quantise> quantise;       // pre-inference into an 8-bit pool: users whose tiles in scratch go into their entries, layer by layer
+  bool reads8 = false;                  // some user's prefix is read from an 8-bit pool
   for (int u = 0; u < n; ++u) {
     UserDesc& ud = users[u];
     memset(&ud, 0, sizeof(ud));
@@ -694,22 +702,29 @@ static int run_typed(relaygr_ctx* c, KvPool* pool, const relaygr_batch* b, Mode 
       PoolEntry e;
       if (pool->resolve(h, &e) != RELAYGR_OK) return fail(RELAYGR_ENOENT, "user %d: stale or unknown handle", u);
       if (e.prefix_len != L) return fail(RELAYGR_EINVAL, "user %d: prefix length %d differs from the cached entry's %d", u, L, e.prefix_len);
-      ud.kv = pool->slab;
-      ud.kv_tile0 = e.page0 * (pool->page_tokens / kTile) * pool->tile_stride;
-      ud.kv_tile_stride = pool->tile_stride;
-      ud.kv_layer_stride = pool->layer_stride;
       compute_prefix = (mode == kPrefill);
+      if (pool->q8 && compute_prefix) {
+        quantise.push_back({u, e.page0});      // K and V are computed as 16-bit tiles in scratch
+      } else {
+        ud.kv = pool->slab;
+        ud.kv_tile0 = e.page0 * (pool->page_tokens / kTile) * pool->tile_stride;
+        ud.kv_tile_stride = pool->tile_stride;
+        ud.kv_layer_stride = pool->layer_stride;
+        reads8 = reads8 || pool->q8;
+      }
     } else {
       if (mode == kPrefill) {
         if (L > 0) return fail(RELAYGR_EINVAL, "prefill: user %d has no handle", u);
         compute_prefix = false;
       } else {
         compute_prefix = L > 0;
-        ud.kv_tile0 = kvs_tiles * (int64_t)(2 * kTile * d);   // pointer filled in once scratch is carved
-        ud.kv_tile_stride = (int64_t)2 * kTile * d;
-        ud.kv_layer_stride = 0;
-        kvs_tiles += (L + kTile - 1) / kTile;
       }
+    }
+    if (!ud.kv && (mode != kPrefill || compute_prefix)) {
+      ud.kv_tile0 = kvs_tiles * (int64_t)(2 * kTile * d);   // pointer filled in once scratch is carved
+      ud.kv_tile_stride = (int64_t)2 * kTile * d;
+      ud.kv_layer_stride = 0;
+      kvs_tiles += (L + kTile - 1) / kTile;
     }
     pstart[u] = (int32_t)prow;
     ud.prow0 = compute_prefix ? (int32_t)prow : -1;
@@ -796,7 +811,12 @@ static int run_typed(relaygr_ctx* c, KvPool* pool, const relaygr_batch* b, Mode 
   for (int u = 0; u < n; ++u)
     if (!users[u].kv) users[u].kv = kvs;
   for (auto* list : {&cut.all, &cut.last})
-    for (AttnTile& a : *list) a.kv = (const char*)users[a.user].kv + users[a.user].kv_tile0 * (int64_t)sizeof(T);
+    for (AttnTile& a : *list) {
+      const UserDesc& ud = users[a.user];
+      a.kv = (const char*)ud.kv + ud.kv_tile0 * (reads8 && ud.kv == pool->slab ? 1 : (int64_t)sizeof(T));
+    }
+  std::vector<TilesJob> to_pool;
+  for (const Quantise& z : quantise) to_pool.push_back({z.page0, (users[z.user].L + kTile - 1) / kTile, (const char*)kvs + users[z.user].kv_tile0 * (int64_t)sizeof(T)});
 
   // -- descriptor blob: users | pstart | nstart | tiles(new, prefix)
   StagingSlot* slot;
@@ -932,6 +952,11 @@ static int run_typed(relaygr_ctx* c, KvPool* pool, const relaygr_batch* b, Mode 
       run_f1(a0, R, all4);
       LAUNCH_CHECK("f1");
     }
+    if (!to_pool.empty()) {
+      ProfScope ps(c, RELAYGR_K_F1, st);
+      rc = quantise_tiles(pool, l, to_pool.data(), (int)to_pool.size(), st);
+      if (rc != RELAYGR_OK) return rc;
+    }
     if (!have_active) continue;
     // step 3: attention partial sums
     AttnParams ap;
@@ -939,6 +964,7 @@ static int run_typed(relaygr_ctx* c, KvPool* pool, const relaygr_batch* b, Mode 
     ap.split_stride = (size_t)R * d; ap.nsplit = p.nsplit; ap.d = d; ap.n_heads = H; ap.layer = l; ap.score_mul = score_mul;
     ap.ml = ml; ap.ml_stride = (size_t)R * H * 2; ap.gs = shared_tiles < kNoneShared ? 2 : cut.gs;
     ap.shared_tiles = shared_tiles;
+    ap.scales_off = reads8 ? q8_scales_off(cfg, l) - l * pool->layer_stride : 0;
     // 16-bit SiLU form: the attention kernel adds the candidates' own keys, so the layer tail does not read q, k, v again
     const bool self_in_attn = bf16 && !softmax;
     ap.knew = self_in_attn ? (const void*)knew : nullptr; ap.vnew = vnew; ap.n_prows = p.n_prows; ap.n_rows = R;
@@ -1068,7 +1094,6 @@ static int run(relaygr_ctx* c, relaygr_kv_pool* pool, const relaygr_batch* b, Mo
     const relaygr_model_config &a = kp->cfg, &m = c->cfg;
     if (a.n_layers != m.n_layers || a.d_model != m.d_model || a.n_heads != m.n_heads || a.dtype != m.dtype)
       return fail(RELAYGR_EINVAL, "pool and context were created for different model shapes");
-    if (kp->q8) return fail(RELAYGR_EINVAL, "the pool holds 8-bit K/V");
   }
   hipStream_t st = (hipStream_t)stream;
   (void)hipGetLastError();   // a failure the caller's own HIP calls left behind is not this call's: launch checks below start clean

@@ -108,6 +108,46 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
              max((uint32_t)__builtin_amdgcn_readlane((int)v, 32), (uint32_t)__builtin_amdgcn_readlane((int)v, 48)));
 }
 
+// Largest finite magnitude of a wavefront's 16-byte pieces of a block.
+template <typename H, int N>
+__device__ __forceinline__ float kv8_top(const uint4 (&x)[N]) {
+  uint32_t top2 = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    top2 = max_u16x2(top2, x[i].x & 0x7FFF7FFFu); top2 = max_u16x2(top2, x[i].y & 0x7FFF7FFFu);
+    top2 = max_u16x2(top2, x[i].z & 0x7FFF7FFFu); top2 = max_u16x2(top2, x[i].w & 0x7FFF7FFFu);
+  }
+  uint32_t top = wave_max_u32(max(top2 & 0xFFFFu, top2 >> 16));
+  if (top >= Fp8<H>::kInf) {     // infinities or NaN among them: leave those out
+    uint32_t t = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t lo = w[j] & 0x7FFFu, hi = (w[j] >> 16) & 0x7FFFu;
+        t = max(t, max(lo >= Fp8<H>::kInf ? 0u : lo, hi >= Fp8<H>::kInf ? 0u : hi));
+      }
+    }
+    top = wave_max_u32(t);
+  }
+  return Fp8<H>::bits_to_f32(top);
+}
+// Eight values to eight codes.
+template <typename H>
+__device__ __forceinline__ uint2 kv8_quantise(const uint4& a, float scale) {
+  if (scale != pow2f(Fp8<H>::kTopExp)) return make_uint2(Fp8<H>::down4(a.x, a.y, scale), Fp8<H>::down4(a.z, a.w, scale));
+  constexpr float inv = Fp8<H>::kTopExp == 8 ? 0x1p-8f : 0x1p-120f;       // 256 * scale would be beyond the type: clamped in fp32
+  float y[8];
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float v = H::of_word(w[i >> 1], i) * inv;
+    y[i] = fabsf(v) > 240.0f && fabsf(v) < 256.0f ? copysignf(240.0f, v) : v;      // (infinities and NaN stay)
+  }
+  return make_uint2(fp8_down4_f32(y[0], y[1], y[2], y[3], 1.0f), fp8_down4_f32(y[4], y[5], y[6], y[7], 1.0f));
+}
+
 // ---- rows into the cache, and back ------------------------------------------------------------------------------------------------
 // The users of a launch travel in the kernel's arguments: no staging, no scratch, nothing for two calls to share.
 constexpr int kRowUsers = 64;
@@ -196,28 +236,7 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(RowsParams p) {
     return n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
   };
 
-  // largest magnitude
-  uint32_t top2 = 0;
-#pragma unroll
-  for (int i = 0; i < NL; ++i) {
-    top2 = max_u16x2(top2, x[i].x & 0x7FFF7FFFu); top2 = max_u16x2(top2, x[i].y & 0x7FFF7FFFu);
-    top2 = max_u16x2(top2, x[i].z & 0x7FFF7FFFu); top2 = max_u16x2(top2, x[i].w & 0x7FFF7FFFu);
-  }
-  uint32_t top = wave_max_u32(max(top2 & 0xFFFFu, top2 >> 16));
-  if (top >= Fp8<H>::kInf) {     // infinities or NaN among them: leave those out
-    uint32_t t = 0;
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t lo = w[j] & 0x7FFFu, hi = (w[j] >> 16) & 0x7FFFu;
-        t = max(t, max(lo >= Fp8<H>::kInf ? 0u : lo, hi >= Fp8<H>::kInf ? 0u : hi));
-      }
-    }
-    top = wave_max_u32(t);
-  }
-  float amax = Fp8<H>::bits_to_f32(top);
+  float amax = kv8_top<H, NL>(x);
   if (u.r0 > 0) {
     uint32_t t = 0;
 #pragma unroll
@@ -234,34 +253,17 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(RowsParams p) {
     const f32x2_t kept_top = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(t, old_scale, false);
     amax = fmaxf(amax, kept_top[0]);
   }
-  const int e = fp8_exponent(amax);
-  const float scale = pow2f(e);
-  const bool top_block = e == Fp8<H>::kTopExp;     // 256 would be beyond the type: through fp32, clamped
-
-  // eight values to eight codes
-  auto quantise = [&](const uint4& a) -> uint2 {
-    if (!top_block) return make_uint2(Fp8<H>::down4(a.x, a.y, scale), Fp8<H>::down4(a.z, a.w, scale));
-    const float inv = pow2f(-e);
-    float y[8];
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float v = H::of_word(w[i >> 1], i) * inv;
-      y[i] = fabsf(v) > 240.0f && fabsf(v) < 256.0f ? copysignf(240.0f, v) : v;      // (infinities and NaN stay)
-    }
-    return make_uint2(fp8_down4_f32(y[0], y[1], y[2], y[3], 1.0f), fp8_down4_f32(y[4], y[5], y[6], y[7], 1.0f));
-  };
-
+  const float scale = pow2f(fp8_exponent(amax));
   uint4 out[NL / 2];
   if (!u.is_v) {
 #pragma unroll
     for (int c = 0; c < NL / 2; ++c) {
-      const uint2 lo = quantise(x[2 * c]), hi = quantise(x[2 * c + 1]);
+      const uint2 lo = kv8_quantise<H>(x[2 * c], scale), hi = kv8_quantise<H>(x[2 * c + 1], scale);
       out[c] = make_uint4(lo.x, lo.y, hi.x, hi.y);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) *reinterpret_cast<uint2*>(lds + tok(i) * LROW + feat(i)) = quantise(x[i]);
+    for (int i = 0; i < NL; ++i) *reinterpret_cast<uint2*>(lds + tok(i) * LROW + feat(i)) = kv8_quantise<H>(x[i], scale);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -292,6 +294,42 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(RowsParams p) {
 #pragma unroll
   for (int c = 0; c < NL / 2; ++c) *reinterpret_cast<uint4*>(codes + (c * 64 + lane) * 16) = out[c];
   if (lane == 0) *scale_at = scale;
+}
+
+// Quantises whole tiles that are already in the order of the 16-bit layout: a pre-inference's K and V of one layer, from its scratch tiles into the
+// pool.  One wavefront a block; a lane's output chunk is its pieces of two consecutive fragments, so that nothing changes lanes.
+struct TilesUser {
+  char* tile0;             // of the pool entry
+  const uint16_t* src;     // the user's tile 0 in scratch, head 0
+  int32_t unit0, pad_;     // tiles of the launch's users before it
+};
+struct TilesParams {
+  int64_t tile_stride, src_stride;   // bytes between the entry's tiles; elements between scratch tiles
+  int64_t codes_off, scales_off;
+  int32_t n_users, n_tiles, n_heads, pad_;
+  TilesUser users[kRowUsers];
+};
+template <typename H, int DH>
+__global__ __launch_bounds__(256) void kv8_tiles_kernel(TilesParams p) {
+  constexpr int NL = DH / 8;
+  const int lane = threadIdx.x & 63;
+  const int unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  const int is_v = unit & 1, t = (unit >> 1) / p.n_heads, head = (unit >> 1) - t * p.n_heads;
+  if (t >= p.n_tiles) return;
+  const int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < p.n_users && p.users[lane < p.n_users ? lane : 0].unit0 <= t)) - 1;
+  const TilesUser& us = p.users[__builtin_amdgcn_readfirstlane(at)];
+  const uint4* src = reinterpret_cast<const uint4*>(us.src + (int64_t)(t - us.unit0) * p.src_stride + (2 * head + is_v) * (kTile * DH));
+  char* tile = us.tile0 + (int64_t)(t - us.unit0) * p.tile_stride;
+  uint4 x[NL];
+#pragma unroll
+  for (int i = 0; i < NL; ++i) x[i] = src[i * 64 + lane];
+  const float scale = pow2f(fp8_exponent(kv8_top<H, NL>(x)));
+#pragma unroll
+  for (int c = 0; c < NL / 2; ++c) {
+    const uint2 lo = kv8_quantise<H>(x[2 * c], scale), hi = kv8_quantise<H>(x[2 * c + 1], scale);
+    *reinterpret_cast<uint4*>(tile + p.codes_off + (2 * head + is_v) * (kTile * DH) + (c * 64 + lane) * 16) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+  }
+  if (lane == 0) reinterpret_cast<float*>(tile + p.scales_off)[2 * head + is_v] = scale;
 }
 
 // Reads: the values that tokens [r0, r1) of the block stand for, into their rows.  One wavefront a block, 1 byte in and 2 out per value.
