@@ -175,8 +175,11 @@ def _dtype_code(dtype: str) -> int:
     return {"fp32": RELAYGR_DTYPE_FP32, "bf16": RELAYGR_DTYPE_BF16, "fp16": RELAYGR_DTYPE_FP16}[dtype]
 
 
+_TORCH_DTYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+
+
 def _torch_dtype(dtype: str):
-    return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
+    return _TORCH_DTYPES[dtype]
 
 
 def make_config(n_layers: int, d_model: int, n_heads: int, dtype: str, ln_eps: float = 1e-5) -> ModelConfigC:
@@ -382,70 +385,79 @@ class KvRows:
             return None if a is None else a.ctypes.data_as(C.POINTER(C.c_int32))
         self.c = KvRowsC(self.n_users, self.handles.ctypes.data_as(C.POINTER(C.c_uint64)), ptr(self.row_off), ptr(self.first_token),
                          ptr(self.key_len))
+        self.ref = C.byref(self.c)
 
 
 def _kv_rows_array(what: str, pool: KvPool, rows: KvRows, t: torch.Tensor):
     """(address, elements between rows) of a tensor [rows, d_model] or [rows, heads, d_head] on the pool's device."""
-    d, heads = pool.cfg.d_model, pool.cfg.n_heads
-    ok = t.dtype == _torch_dtype(pool.dtype) and t.device == pool.slab.device and t.shape[0] == rows.n_rows
-    if t.dim() == 2:
-        ok = ok and t.shape[1] == d and t.stride(1) == 1
+    d, n, shape, stride = pool.cfg.d_model, rows.n_rows, t.shape, t.stride()
+    if len(shape) == 2:
+        ok = shape[0] == n and shape[1] == d and stride[1] == 1
     else:
-        ok = ok and t.dim() == 3 and t.shape[1:] == (heads, d // heads) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == d // heads)
-    if not ok:
-        raise RelayGRError(RELAYGR_EINVAL, f"{what}: needs {rows.n_rows} rows of {d} adjacent {pool.dtype} elements on {pool.slab.device}, got "
-                                           f"{tuple(t.shape)} of {t.dtype} on {t.device} with strides {t.stride()}")
+        heads = pool.cfg.n_heads
+        ok = len(shape) == 3 and tuple(shape) == (n, heads, d // heads) and stride[2] == 1 and (heads == 1 or stride[1] == d // heads)
+    if not ok or t.dtype != _torch_dtype(pool.dtype) or t.device != pool.slab.device:
+        raise RelayGRError(RELAYGR_EINVAL, f"{what}: needs {n} rows of {d} adjacent {pool.dtype} elements on {pool.slab.device}, got "
+                                           f"{tuple(shape)} of {t.dtype} on {t.device} with strides {stride}")
     # (the stride of a single row means nothing: torch may report any)
-    return (t.data_ptr() if rows.n_rows else None), (t.stride(0) if rows.n_rows > 1 else d)
+    return (t.data_ptr() if n else None), (stride[0] if n > 1 else d)
 
 
-def _on_stream(pool: KvPool, stream):
-    """The stream of a call (default: the current one of the pool's device), as a torch stream and as a raw handle."""
-    if stream is None:
-        s = torch.cuda.current_stream(pool.slab.device)
-        return s, s.cuda_stream
-    if isinstance(stream, int):
-        return torch.cuda.ExternalStream(stream, device=pool.slab.device), stream
-    return stream, stream.cuda_stream
+class _KvCall:
+    """Where a call's work and results go: a stream (default: the current one of the pool's device), with that device current.  Entered only
+    where the caller's state is not that already: torch's guards take several microseconds."""
+
+    def __init__(self, pool: KvPool, stream):
+        device = pool.slab.device
+        if stream is None:
+            self.raw = torch._C._cuda_getCurrentRawStream(device.index)
+            self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+        else:
+            s = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
+            self.raw, self.guard = s.cuda_stream, torch.cuda.stream(s)      # (results are allocated on the stream that writes them)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self.raw
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
 
 
-def _new_rows(pool: KvPool, rows: KvRows, stream) -> torch.Tensor:
-    """A result's memory, taken on the stream that writes it."""
-    with torch.cuda.stream(stream):
-        return torch.empty((rows.n_rows, pool.cfg.d_model), dtype=_torch_dtype(pool.dtype), device=pool.slab.device)
+def _new_rows(pool: KvPool, rows: KvRows) -> torch.Tensor:
+    return torch.empty((rows.n_rows, pool.cfg.d_model), dtype=_torch_dtype(pool.dtype), device=pool.slab.device)
 
 
 def relaygr_kv_pool_write(pool: KvPool, layer: int, rows: KvRows, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
     """Quantises rows of K and V ([rows, d_model] or [rows, heads, d_head]) into the entries' tokens first_token on."""
     kp, ks = _kv_rows_array("kv_pool_write: k", pool, rows, k)
     vp, vs = _kv_rows_array("kv_pool_write: v", pool, rows, v)
-    _, st = _on_stream(pool, stream)
-    with torch.cuda.device(pool.slab.device):
-        _check(load_library().relaygr_kv_pool_write(pool.handle, layer, C.byref(rows.c), kp, ks, vp, vs, st))
+    with _KvCall(pool, stream) as st:
+        _check(load_library().relaygr_kv_pool_write(pool.handle, layer, rows.ref, kp, ks, vp, vs, st))
 
 
 def relaygr_kv_pool_read(pool: KvPool, layer: int, rows: KvRows, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
                          stream=None):
     """(k, v): the values that tokens of the entries stand for, [rows, d_model] each (made here if not given)."""
-    ts, st = _on_stream(pool, stream)
-    k = _new_rows(pool, rows, ts) if k is None else k
-    v = _new_rows(pool, rows, ts) if v is None else v
-    kp, ks = _kv_rows_array("kv_pool_read: k", pool, rows, k)
-    vp, vs = _kv_rows_array("kv_pool_read: v", pool, rows, v)
-    with torch.cuda.device(pool.slab.device):
-        _check(load_library().relaygr_kv_pool_read(pool.handle, layer, C.byref(rows.c), kp, ks, vp, vs, st))
+    with _KvCall(pool, stream) as st:
+        k = _new_rows(pool, rows) if k is None else k
+        v = _new_rows(pool, rows) if v is None else v
+        kp, ks = _kv_rows_array("kv_pool_read: k", pool, rows, k)
+        vp, vs = _kv_rows_array("kv_pool_read: v", pool, rows, v)
+        _check(load_library().relaygr_kv_pool_read(pool.handle, layer, rows.ref, kp, ks, vp, vs, st))
     return k, v
 
 
 def relaygr_cache_attend(ctx: Context, pool: KvPool, layer: int, rows: KvRows, q: torch.Tensor, causal: bool = False,
                          out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """One layer's attention of query rows over entries of an 8-bit pool, in the context's form: [rows, d_model] (made here if not given)."""
-    ts, st = _on_stream(pool, stream)
-    out = _new_rows(pool, rows, ts) if out is None else out
     qp, qs = _kv_rows_array("cache_attend: q", pool, rows, q)
-    op, os_ = _kv_rows_array("cache_attend: out", pool, rows, out)
-    with torch.cuda.device(pool.slab.device):
-        _check(load_library().relaygr_cache_attend(ctx.handle, pool.handle, layer, C.byref(rows.c), int(causal), qp, qs, op, os_, st))
+    with _KvCall(pool, stream) as st:
+        out = _new_rows(pool, rows) if out is None else out
+        op, os_ = _kv_rows_array("cache_attend: out", pool, rows, out)
+        _check(load_library().relaygr_cache_attend(ctx.handle, pool.handle, layer, rows.ref, int(causal), qp, qs, op, os_, st))
     return out
 
 

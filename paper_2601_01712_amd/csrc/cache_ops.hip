@@ -45,8 +45,54 @@ int resolve_rows(const char* what, KvPool* pool, int32_t layer, const relaygr_kv
   return RELAYGR_OK;
 }
 
+// launch(storage type, d_head)
+template <class F>
+void by_head(const relaygr_model_config& cfg, F launch) {
+  auto by_dh = [&](auto h) {
+    switch (cfg.d_model / cfg.n_heads) {
+      case 32: launch(h, std::integral_constant<int, 32>()); break;
+      case 64: launch(h, std::integral_constant<int, 64>()); break;
+      default: launch(h, std::integral_constant<int, 128>()); break;
+    }
+  };
+  if (cfg.dtype == RELAYGR_DTYPE_FP16) by_dh(F16());
+  else by_dh(Bf16());
+}
+
 char* entry_tile0(const KvPool* pool, const PoolEntry& e) {
   return (char*)pool->slab + (size_t)e.page0 * pool->page_bytes;
+}
+
+template <bool WRITE, int USERS>
+int launch_rows(const char* what, const KvPool* pool, int layer, const relaygr_kv_rows* r, const std::vector<PoolEntry>& entries, void* k, int64_t k_stride,
+                void* v, int64_t v_stride, hipStream_t st) {
+  const relaygr_model_config& cfg = pool->cfg;
+  RowsParams<USERS> p = {};
+  p.k = k; p.v = v; p.k_stride = k_stride; p.v_stride = v_stride;
+  p.tile_stride = pool->tile_stride;
+  p.codes_off = layer * pool->layer_stride;
+  p.scales_off = q8_scales_off(cfg, layer);
+  p.n_heads = cfg.n_heads;
+  for (int u = 0; u < r->n_users;) {
+    p.n_users = 0; p.n_tiles = 0;
+    for (; u < r->n_users && p.n_users < USERS; ++u) {
+      const int32_t first = r->first_token ? r->first_token[u] : 0, n = r->row_off[u + 1] - r->row_off[u];
+      if (n == 0) continue;
+      p.users[p.n_users++] = {entry_tile0(pool, entries[u]), first, n, r->row_off[u], p.n_tiles, 0};
+      p.n_tiles += (int)(((int64_t)first + n - 1) / kTile - first / kTile + 1);
+    }
+    if (p.n_users == 0) break;
+    const dim3 grid((unsigned)(((int64_t)p.n_tiles * cfg.n_heads * 2 + 3) / 4));
+    auto launch = [&](auto h, auto dim) {
+      using H = decltype(h);
+      constexpr int DH = decltype(dim)::value;
+      if (WRITE) hipLaunchKernelGGL((kv8_write_kernel<H, DH, USERS>), grid, dim3(256), 0, st, p);
+      else hipLaunchKernelGGL((kv8_read_kernel<H, DH, USERS>), grid, dim3(256), 0, st, p);
+    };
+    by_head(cfg, launch);
+    LAUNCH_CHECK(what);
+  }
+  return RELAYGR_OK;
 }
 
 template <bool WRITE>
@@ -70,42 +116,8 @@ int move_rows(const char* what, KvPool* pool, int32_t layer, const relaygr_kv_ro
     if (std::adjacent_find(hs.begin(), hs.end()) != hs.end()) return fail(RELAYGR_EINVAL, "%s: two users of the batch carry the same handle", what);
   }
   (void)hipGetLastError();   // a failure the caller's own HIP calls left behind is not this call's
-  RowsParams p = {};
-  p.k = k; p.v = v; p.k_stride = k_stride; p.v_stride = v_stride;
-  p.tile_stride = pool->tile_stride;
-  p.codes_off = layer * pool->layer_stride;
-  p.scales_off = q8_scales_off(cfg, layer);
-  p.n_heads = cfg.n_heads;
-  const int dh = cfg.d_model / cfg.n_heads;
-  for (int u = 0; u < r->n_users;) {
-    p.n_users = 0; p.n_tiles = 0;
-    for (; u < r->n_users && p.n_users < kRowUsers; ++u) {
-      const int32_t first = r->first_token ? r->first_token[u] : 0, n = r->row_off[u + 1] - r->row_off[u];
-      if (n == 0) continue;
-      p.users[p.n_users++] = {entry_tile0(pool, entries[u]), first, n, r->row_off[u], p.n_tiles, 0};
-      p.n_tiles += (int)(((int64_t)first + n - 1) / kTile - first / kTile + 1);
-    }
-    if (p.n_users == 0) break;
-    const int64_t units = (int64_t)p.n_tiles * cfg.n_heads * 2;
-    const dim3 grid((unsigned)((units + 3) / 4));
-    auto launch = [&](auto h, auto dim) {
-      using H = decltype(h);
-      constexpr int DH = decltype(dim)::value;
-      if (WRITE) hipLaunchKernelGGL((kv8_write_kernel<H, DH>), grid, dim3(256), 0, st, p);
-      else hipLaunchKernelGGL((kv8_read_kernel<H, DH>), grid, dim3(256), 0, st, p);
-    };
-    auto by_dh = [&](auto h) {
-      switch (dh) {
-        case 32: launch(h, std::integral_constant<int, 32>()); break;
-        case 64: launch(h, std::integral_constant<int, 64>()); break;
-        default: launch(h, std::integral_constant<int, 128>()); break;
-      }
-    };
-    if (cfg.dtype == RELAYGR_DTYPE_FP16) by_dh(F16());
-    else by_dh(Bf16());
-    LAUNCH_CHECK(what);
-  }
-  return RELAYGR_OK;
+  if (r->n_users <= kFewRowUsers) return launch_rows<WRITE, kFewRowUsers>(what, pool, layer, r, entries, k, k_stride, v, v_stride, st);
+  return launch_rows<WRITE, kRowUsers>(what, pool, layer, r, entries, k, k_stride, v, v_stride, st);
 }
 
 template <typename H, bool SM>
@@ -130,7 +142,7 @@ void launch_attend(const AttendParams& p, int dh, bool wide, int rows, int row_b
 
 int relaygr::quantise_tiles(const KvPool* pool, int layer, const TilesJob* jobs, int n_jobs, hipStream_t st) {
   const relaygr_model_config& cfg = pool->cfg;
-  const int d = cfg.d_model, dh = d / cfg.n_heads;
+  const int d = cfg.d_model;
   TilesParams p = {};
   p.tile_stride = pool->tile_stride; p.src_stride = (int64_t)2 * kTile * d;
   p.codes_off = layer * pool->layer_stride; p.scales_off = q8_scales_off(cfg, layer); p.n_heads = cfg.n_heads;
@@ -141,16 +153,7 @@ int relaygr::quantise_tiles(const KvPool* pool, int layer, const TilesJob* jobs,
       p.n_tiles += jobs[j].tiles;
     }
     const dim3 grid((unsigned)(((int64_t)p.n_tiles * cfg.n_heads * 2 + 3) / 4));
-    auto by_dh = [&](auto h) {
-      using H = decltype(h);
-      switch (dh) {
-        case 32: hipLaunchKernelGGL((kv8_tiles_kernel<H, 32>), grid, dim3(256), 0, st, p); break;
-        case 64: hipLaunchKernelGGL((kv8_tiles_kernel<H, 64>), grid, dim3(256), 0, st, p); break;
-        default: hipLaunchKernelGGL((kv8_tiles_kernel<H, 128>), grid, dim3(256), 0, st, p); break;
-      }
-    };
-    if (cfg.dtype == RELAYGR_DTYPE_FP16) by_dh(F16());
-    else by_dh(Bf16());
+    by_head(cfg, [&](auto h, auto dim) { hipLaunchKernelGGL((kv8_tiles_kernel<decltype(h), decltype(dim)::value>), grid, dim3(256), 0, st, p); });
     LAUNCH_CHECK("kv8_tiles");
   }
   return RELAYGR_OK;

@@ -149,8 +149,9 @@ __device__ __forceinline__ uint2 kv8_quantise(const uint4& a, float scale) {
 }
 
 // ---- rows into the cache, and back ------------------------------------------------------------------------------------------------
-// The users of a launch travel in the kernel's arguments: no staging, no scratch, nothing for two calls to share.
-constexpr int kRowUsers = 64;
+// The users of a launch travel in the kernel's arguments: no staging, no scratch, nothing for two calls to share.  A launch with 2.6 KB of
+// arguments takes 4.3 us of the host, one with 650 bytes 3.2, so that launches of few users take kernels with room for few.
+constexpr int kRowUsers = 64, kFewRowUsers = 14;
 struct RowsUser {
   char* tile0;       // the user's tile 0 (all layers)
   int32_t first;     // token that the user's first row is
@@ -159,14 +160,14 @@ struct RowsUser {
   int32_t unit0;     // touched tiles of the launch's users before it
   int32_t pad_;
 };
-struct RowsParams {
+template <int USERS> struct RowsParams {
   void* k;           // [rows][stride] in the storage type: sources of a write, targets of a read
   void* v;
   int64_t k_stride, v_stride;   // elements between rows
   int64_t tile_stride;          // bytes between the tiles of an entry
   int64_t codes_off, scales_off;   // of the layer in a tile
   int32_t n_users, n_tiles, n_heads, pad_;
-  RowsUser users[kRowUsers];
+  RowsUser users[USERS];
 };
 
 // A wavefront's unit of a launch: the K or the V block of one head in one touched tile.
@@ -176,7 +177,8 @@ struct RowsUnit {
   int64_t row;        // row that token r0 is
   char* tile;
 };
-__device__ __forceinline__ bool rows_unit(const RowsParams& p, int lane, RowsUnit* u) {
+template <int USERS>
+__device__ __forceinline__ bool rows_unit(const RowsParams<USERS>& p, int lane, RowsUnit* u) {
   const int unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
   u->is_v = unit & 1;
   const int t = (unit >> 1) / p.n_heads;
@@ -196,8 +198,8 @@ __device__ __forceinline__ bool rows_unit(const RowsParams& p, int lane, RowsUni
 // One wavefront a block.  What bounds it is HBM: 2 bytes in and 1 out per value.  K rows are loaded in the order of the codes (a lane's
 // 16 codes are two 16-byte runs of one token); V codes have their lanes along the features and 16 tokens to a lane, so that V goes through LDS
 // as bytes, [token][feature].
-template <typename H, int DH>
-__global__ __launch_bounds__(256) void kv8_write_kernel(RowsParams p) {
+template <typename H, int DH, int USERS>
+__global__ __launch_bounds__(256) void kv8_write_kernel(RowsParams<USERS> p) {
   constexpr int NL = DH / 8;                 // 16-byte loads of a lane: a block is 64 * DH values
   constexpr int LROW = DH + 8;               // bytes between tokens in LDS
   __shared__ __attribute__((aligned(16))) uint8_t turn[2][kTile * LROW];
@@ -333,8 +335,8 @@ __global__ __launch_bounds__(256) void kv8_tiles_kernel(TilesParams p) {
 }
 
 // Reads: the values that tokens [r0, r1) of the block stand for, into their rows.  One wavefront a block, 1 byte in and 2 out per value.
-template <typename H, int DH>
-__global__ __launch_bounds__(256) void kv8_read_kernel(RowsParams p) {
+template <typename H, int DH, int USERS>
+__global__ __launch_bounds__(256) void kv8_read_kernel(RowsParams<USERS> p) {
   constexpr int NL = DH / 8, LROW = DH + 8;
   __shared__ __attribute__((aligned(16))) uint8_t turn[2][kTile * LROW];
   const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
