@@ -11,94 +11,168 @@
 
 namespace relaygr {
 
-constexpr int kAttendUsers = 64;       // of a launch: they travel in the kernel's arguments
+// Users of a launch: they travel in the kernel's arguments, as RowsParams' do.
+constexpr int kAttendUsers = 128, kFewAttendUsers = 16;
 constexpr int kAttendWaves = 4;        // wavefronts of a workgroup
 struct AttendUser {
-  const char* kv;      // codes of the entry's tile 0, head 0, in the call's layer
+  int32_t page0;       // the entry's first page in the slab
   int32_t row0, rows;  // the user's rows in q and out
   int32_t keys;        // tokens that its last row sees (without `causal`: every row)
   int32_t item0;       // items of the launch's users before it, for one head
   int32_t part0;       // first of its rows in the table of partial sums
-  int32_t parts, per;  // pieces of its key sequence, key tiles in each
-  int32_t pad_;
+  uint32_t cut;        // pieces of its key sequence (7 bits), key tiles in each
+  __host__ __device__ __forceinline__ int parts() const { return (int)(cut & 127); }
+  __host__ __device__ __forceinline__ int per() const { return (int)(cut >> 7); }
 };
-static_assert(sizeof(AttendUser) == 40, "AttendUser layout");
-struct AttendParams {
+static_assert(sizeof(AttendUser) == 28, "AttendUser layout");
+template <int USERS> struct AttendParams {
   const uint16_t* q;
   uint16_t* out;
   int64_t q_stride, out_stride;      // elements between rows
-  int64_t tile_stride, scales_off;   // bytes: between tiles, from a tile's codes to its layer's scales
+  const char* slab;                  // of the pool, at the call's layer
+  int64_t page_bytes, tile_stride, scales_off;   // bytes: of a page, between tiles, from a tile's codes to its layer's scales
   float* part;                       // [partial rows][d] sums of rows that are cut along the keys
   float* ml;                         // softmax form: [partial rows][n_heads][2] reference score (log2 units) and sum of weights
   int32_t n_users, n_items, d, n_heads, causal;
   float score_mul;                   // alpha * log2(e)
-  AttendUser users[kAttendUsers];
+  AttendUser users[USERS];
 };
 // Tokens that row i of the user sees.
 __device__ __forceinline__ int attend_seen(const AttendUser& u, int i, int causal) { return causal ? max(u.keys - u.rows + 1 + i, 0) : u.keys; }
 
+template <bool ONCE>
+__device__ __forceinline__ uint4 load16(const char* p) {
+  const u32x4_t* x = reinterpret_cast<const u32x4_t*>(p);
+  return __builtin_bit_cast(uint4, ONCE ? __builtin_nontemporal_load(x) : *x);
+}
+
 // NaN codes of four, as 0x01 in their bytes.
 __device__ __forceinline__ uint32_t fp8_nans(uint32_t codes) { return (((codes & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u; }
 
-// A tile that not every row sees whole: a weight of zero is no answer to a NaN in V (0 * NaN), which only rows that see its token may get.  Where a
-// tile holds any, they leave the tile's V, and what is NaN times what is seen is added twice to the sums, as +inf and as -inf: products
-// of powers of two beyond fp32 (in bf16 whatever the storage type; fp16 does not reach that far).
-template <int NQ, int DB>
-__device__ __forceinline__ void attend8_nans(uint4 (&vr)[DB][2], f32x16_t (&oacc)[DB][NQ], const int (&vis)[NQ]) {
+// A tile that not every row sees whole: a weight of zero is no answer to a NaN in V (0 * NaN), which only rows that see its token may get.  NaN codes
+// leave the V that the weights are multiplied with, and what is NaN times what is seen is added twice to the sums, as +inf and as -inf: products
+// of powers of two beyond fp32 (in bf16 whatever the storage type; fp16 does not reach that far).  `chunk`: V codes (db, kb); vis: tokens of the tile
+// that the lane's rows see, less 4g.
+template <int NQ>
+__device__ __forceinline__ void attend8_nans(uint4& chunk, int kb, f32x16_t (&o)[NQ], const int (&vis)[NQ]) {
   const uint32_t big = 0x7180;          // 2^100 in bf16
 #pragma unroll
-  for (int kb = 0; kb < 2; ++kb)
+  for (int m = 0; m < 2; ++m) {
+    uint32_t &w0 = m == 0 ? chunk.x : chunk.z, &w1 = m == 0 ? chunk.y : chunk.w;
+    const uint32_t n0 = fp8_nans(w0), n1 = fp8_nans(w1);
+    w0 &= ~(n0 * 0xFFu);
+    w1 &= ~(n1 * 0xFFu);
+    const u32x4_t pos = fp8_frag<Bf16>(n0 * 0x38u, n1 * 0x38u, 0x1p100f), neg = fp8_frag<Bf16>(n0 * 0xB8u, n1 * 0xB8u, 0x1p100f);   // codes of 1 and -1
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int qb = 0; qb < NQ; ++qb) {
+      uint32_t see[4];
 #pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        uint32_t w0 = m == 0 ? vr[db][kb].x : vr[db][kb].z, w1 = m == 0 ? vr[db][kb].y : vr[db][kb].w;
-        const uint32_t n0 = fp8_nans(w0), n1 = fp8_nans(w1);
-        w0 &= ~(n0 * 0xFFu); w1 &= ~(n1 * 0xFFu);
-        if (m == 0) { vr[db][kb].x = w0; vr[db][kb].y = w1; } else { vr[db][kb].z = w0; vr[db][kb].w = w1; }
-        const u32x4_t pos = fp8_frag<Bf16>(n0 * 0x38u, n1 * 0x38u, 0x1p100f), neg = fp8_frag<Bf16>(n0 * 0xB8u, n1 * 0xB8u, 0x1p100f);   // codes of 1 and -1
-#pragma unroll
-        for (int qb = 0; qb < NQ; ++qb) {
-          uint32_t see[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int e = 8 * m + 2 * j, key = kb * 32 + 8 * (e >> 2) + (e & 3);
-            see[j] = (key < vis[qb] ? big : 0u) | (key + 1 < vis[qb] ? big << 16 : 0u);
-          }
-          const uint4 sees = make_uint4(see[0], see[1], see[2], see[3]);
-          oacc[db][qb] = Bf16::mfma(neg, sees, Bf16::mfma(pos, sees, oacc[db][qb]));
-        }
-        __builtin_amdgcn_sched_barrier(0);
+      for (int j = 0; j < 4; ++j) {
+        const int e = 8 * m + 2 * j, key = kb * 32 + 8 * (e >> 2) + (e & 3);
+        see[j] = (key < vis[qb] ? big : 0u) | (key + 1 < vis[qb] ? big << 16 : 0u);
       }
+      const uint4 sees = make_uint4(see[0], see[1], see[2], see[3]);
+      o[qb] = Bf16::mfma(neg, sees, Bf16::mfma(pos, sees, o[qb]));
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// An item of the launch: rows of one user, one head, one piece of the key sequence.
+struct AttendItem {
+  AttendUser u;
+  int head, piece, first_row, n_rows;
+  int most, least;      // tokens that the last and the first of its rows see
+  int t0, t1;           // key tiles
+};
+// The workgroup's item (ROWS to an item); false: it has none.  Heads are dealt to the XCDs as in attention.h, so that the row tiles of one user and
+// head share an L2.
+template <int ROWS, int USERS>
+__device__ __forceinline__ bool attend8_item(const AttendParams<USERS>& p, int lane, AttendItem* it) {
+  const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, heads_sh = __builtin_ctz(p.n_heads);
+  int item;
+  if (p.n_heads >= 8) {
+    const int sh = heads_sh - 3;
+    it->head = (xcd << sh) + (turn & ((1 << sh) - 1));
+    item = turn >> sh;
+  } else {
+    it->head = xcd & (p.n_heads - 1);
+    item = (turn << (3 - heads_sh)) + (xcd >> heads_sh);
+  }
+  if (item >= p.n_items) return false;
+  int at = -1;                     // the last user whose items begin at or before this one
+#pragma unroll
+  for (int u0 = 0; u0 < USERS; u0 += 64) {
+    const bool there = u0 + lane < p.n_users;
+    at += __builtin_popcountll(__builtin_amdgcn_ballot_w64(there && p.users[there ? u0 + lane : 0].item0 <= item));
+  }
+  it->u = p.users[__builtin_amdgcn_readfirstlane(at)];
+  const int row_tiles = (it->u.rows + ROWS - 1) / ROWS;
+  it->piece = (item - it->u.item0) / row_tiles;
+  it->first_row = (item - it->u.item0 - it->piece * row_tiles) * ROWS;
+  it->n_rows = min(ROWS, it->u.rows - it->first_row);
+  it->most = attend_seen(it->u, it->first_row + it->n_rows - 1, p.causal);
+  it->least = attend_seen(it->u, it->first_row, p.causal);
+  it->t0 = it->piece * it->u.per();
+  it->t1 = min(it->t0 + it->u.per(), (it->most + kTile - 1) / kTile);
+  return true;
+}
+
+// Writes a wavefront's 32 * NQ rows: sums over all their keys as outputs, sums of one piece as partial sums.  Element e of o[db][qb]: feature
+// db*32 + 8*(e/4) + 4*g + e%4, row qb*32 + l32 of the wavefront's.
+template <typename H, int DH, int NQ, bool SOFTMAX, int USERS>
+__device__ __forceinline__ void attend8_store(const AttendParams<USERS>& p, const AttendItem& it, int row0, int lane, const int (&seen)[NQ], f32x16_t (&o)[DH / 32][NQ],
+                                              const float (&mref)[NQ], const float (&lane_sum)[NQ]) {
+  constexpr int DB = DH / 32;
+  const int l32 = lane & 31, g = lane >> 5;
+#pragma unroll
+  for (int qb = 0; qb < NQ; ++qb) {
+    const int r = row0 + qb * 32 + l32;
+    const float lsum = SOFTMAX ? lane_sum[qb] + __shfl_xor(lane_sum[qb], 32, 64) : 0.f;
+    if (r >= it.n_rows) continue;
+    if (it.u.parts() == 1) {
+      const float mul = SOFTMAX ? 1.0f / lsum : 0.69314718055994531f / (float)seen[qb];
+      uint16_t* dst = p.out + (int64_t)(it.u.row0 + it.first_row + r) * p.out_stride + it.head * DH + 4 * g;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+          uint2 w = make_uint2(H::pack2(o[db][qb][4 * e4] * mul, o[db][qb][4 * e4 + 1] * mul), H::pack2(o[db][qb][4 * e4 + 2] * mul, o[db][qb][4 * e4 + 3] * mul));
+          if (seen[qb] == 0) w = make_uint2(0, 0);
+          *reinterpret_cast<uint2*>(dst + db * 32 + 8 * e4) = w;
+        }
+    } else {
+      const int64_t pr = (int64_t)it.u.part0 + (int64_t)it.piece * it.u.rows + it.first_row + r;
+      float* dst = p.part + pr * p.d + it.head * DH + 4 * g;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4)
+          *reinterpret_cast<float4*>(dst + db * 32 + 8 * e4) = make_float4(o[db][qb][4 * e4], o[db][qb][4 * e4 + 1], o[db][qb][4 * e4 + 2], o[db][qb][4 * e4 + 3]);
+      if constexpr (SOFTMAX) {
+        if (g == 0) *reinterpret_cast<float2*>(p.ml + (pr * p.n_heads + it.head) * 2) = make_float2(mref[qb], lsum);
+      }
+    }
+  }
 }
 
 // One item: up to 32*NQ rows of one user, one head, one piece of the key sequence.  The workgroup's wavefronts take the piece's key tiles in turn, all
 // for the same rows, each straight from memory to its registers (the codes are in operand order) with the next tile on its way while it
 // works on one; their sums meet in LDS at the end.
-template <typename H, int DH, int NQ, bool SOFTMAX>
-__global__ __launch_bounds__(kAttendWaves * 64, 2) void attend8_kernel(AttendParams p) {
+//
+// ONCE: no other item reads the same codes, and the launch reads more than the caches hold: the loads do not leave them there (128 users of 8192 keys, one row
+// each, d = 512: 1.07 GB in 188 us, with the hint 167).
+template <typename H, int DH, int NQ, bool SOFTMAX, bool ONCE, int USERS>
+__global__ __launch_bounds__(kAttendWaves * 64, 2) void attend8_kernel(AttendParams<USERS> p) {
   constexpr int KS = DH / 16, KP = DH / 32, DB = DH / 32;
   constexpr int BLOCK = kTile * DH;            // bytes of codes of K, and of V
   __shared__ float join[kAttendWaves / 2][(DB * NQ * 16 + (SOFTMAX ? 2 * NQ : 0)) * 64];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // (heads dealt to the XCDs as in attention.h, so that the row tiles of one user and head share an L2)
-  const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, heads_sh = __builtin_ctz(p.n_heads);
-  int head, item;
-  if (p.n_heads >= 8) {
-    const int sh = heads_sh - 3;
-    head = (xcd << sh) + (turn & ((1 << sh) - 1));
-    item = turn >> sh;
-  } else {
-    head = xcd & (p.n_heads - 1);
-    item = (turn << (3 - heads_sh)) + (xcd >> heads_sh);
-  }
-  if (item >= p.n_items) return;
-  const int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < p.n_users && p.users[lane < p.n_users ? lane : 0].item0 <= item)) - 1;
-  const AttendUser u = p.users[__builtin_amdgcn_readfirstlane(at)];
-  const int row_tiles = (u.rows + 32 * NQ - 1) / (32 * NQ);
-  const int piece = (item - u.item0) / row_tiles, first_row = (item - u.item0 - piece * row_tiles) * 32 * NQ;
-  const int n_rows = min(32 * NQ, u.rows - first_row);
+  AttendItem it;
+  if (!attend8_item<32 * NQ>(p, lane, &it)) return;
+  const AttendUser& u = it.u;
+  const int head = it.head, first_row = it.first_row, n_rows = it.n_rows, least = it.least, t0 = it.t0, t1 = it.t1;
 
   int seen[NQ];
   uint4 qf[NQ][KS];
@@ -111,9 +185,6 @@ __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend8_kernel(AttendPar
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[qb][ks] = *reinterpret_cast<const uint4*>(qr + ks * 16);
   }
-  const int most = attend_seen(u, first_row + n_rows - 1, p.causal), least = attend_seen(u, first_row, p.causal);   // of the item's rows
-  const int t0 = piece * u.per, t1 = min(t0 + u.per, (most + kTile - 1) / kTile);
-
   f32x16_t oacc[DB][NQ];
   float mref[NQ], lsum[NQ];
 #pragma unroll
@@ -125,147 +196,138 @@ __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend8_kernel(AttendPar
       for (int e = 0; e < 16; ++e) oacc[db][qb][e] = 0.f;
   }
 
-  const char* base = u.kv + (int64_t)head * (2 * BLOCK);
-  const char* scales = u.kv + p.scales_off + head * 8;
-  uint4 kr[2][KP], vr[DB][2];
+  const char* kv = p.slab + (int64_t)u.page0 * p.page_bytes;
+  const char* base = kv + (int64_t)head * (2 * BLOCK);
+  const char* scales = kv + p.scales_off + head * 8;
+  uint4 kr[2][KP], vr[2][DB];                   // codes of the tile's two halves
   float2 sc;
-  auto load = [&](int t, uint4 (&kx)[2][KP], uint4 (&vx)[DB][2], float2& s) {
+  auto load_k = [&](int t, int kb) {
     const char* tile = base + (int64_t)t * p.tile_stride;
-    s = *reinterpret_cast<const float2*>(scales + (int64_t)t * p.tile_stride);
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int kp = 0; kp < KP; ++kp) kx[kb][kp] = *reinterpret_cast<const uint4*>(tile + (kb * KP + kp) * 1024 + lane * 16);
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) vx[db][kb] = *reinterpret_cast<const uint4*>(tile + BLOCK + (db * 2 + kb) * 1024 + lane * 16);
+    for (int kp = 0; kp < KP; ++kp) kr[kb][kp] = load16<ONCE>(tile + (kb * KP + kp) * 1024 + lane * 16);
   };
-  int t = t0 + wave;
-  if (t < t1) load(t, kr, vr, sc);
-  for (; t < t1; t += kAttendWaves) {
-    uint4 kn[2][KP], vn[DB][2];
-    float2 sn = sc;
+  auto load_v = [&](int t, int kb) {
+    const char* tile = base + (int64_t)t * p.tile_stride + BLOCK;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) vr[kb][db] = load16<ONCE>(tile + (db * 2 + kb) * 1024 + lane * 16);
+  };
+  auto load_scales = [&](int t) { return *reinterpret_cast<const float2*>(scales + (int64_t)t * p.tile_stride); };
+
+  // one tile, half by half; each piece of codes makes room for the wavefront's next tile as soon as it has been converted
+  auto tile = [&](auto more_tag, int t) {
+    constexpr bool MORE = decltype(more_tag)::value;
     const int tn = t + kAttendWaves;
-    load(tn < t1 ? tn : t, kn, vn, sn);
-    // first product: the tile's 64 keys
-    f32x16_t s[2][NQ];
+    float2 sn = sc;
+    if constexpr (MORE) sn = load_scales(tn);
+    const bool masked = least < (t + 1) * kTile;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
+      f32x16_t s[NQ];
 #pragma unroll
       for (int qb = 0; qb < NQ; ++qb)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[kb][qb][e] = 0.f;
+        for (int e = 0; e < 16; ++e) s[qb][e] = 0.f;
 #pragma unroll
       for (int kp = 0; kp < KP; ++kp) {
         const u32x4_t lo = fp8_frag<H>(kr[kb][kp].x, kr[kb][kp].y, sc.x), hi = fp8_frag<H>(kr[kb][kp].z, kr[kb][kp].w, sc.x);
 #pragma unroll
-        for (int qb = 0; qb < NQ; ++qb) s[kb][qb] = H::mfma(lo, qf[qb][2 * kp], s[kb][qb]);
+        for (int qb = 0; qb < NQ; ++qb) s[qb] = H::mfma(lo, qf[qb][2 * kp], s[qb]);
 #pragma unroll
-        for (int qb = 0; qb < NQ; ++qb) s[kb][qb] = H::mfma(hi, qf[qb][2 * kp + 1], s[kb][qb]);
+        for (int qb = 0; qb < NQ; ++qb) s[qb] = H::mfma(hi, qf[qb][2 * kp + 1], s[qb]);
       }
-    }
-    // weights.  Element e of half kb is key kb*32 + 8*(e/4) + 4*g + e%4 of the tile
-    const bool masked = least < (t + 1) * kTile;
-    if (masked) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      if constexpr (MORE) load_k(tn, kb);
+      __builtin_amdgcn_sched_barrier(0);
+      // element e is key kb*32 + 8*(e/4) + 4*g + e%4 of the tile
+      if (masked) {
+        uint32_t any = 0;
 #pragma unroll
         for (int qb = 0; qb < NQ; ++qb) {
           const int vis = seen[qb] - t * kTile - kb * 32 - 4 * g;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s[kb][qb][e] = 8 * (e >> 2) + (e & 3) < vis ? s[kb][qb][e] : (SOFTMAX ? -INFINITY : 0.f);   // (SiLU(0) = 0)
+          for (int e = 0; e < 16; ++e) s[qb][e] = 8 * (e >> 2) + (e & 3) < vis ? s[qb][e] : (SOFTMAX ? -INFINITY : 0.f);   // (SiLU(0) = 0)
         }
-    }
-    uint32_t pk[2][NQ][8];
-    if constexpr (SOFTMAX) {
-      // the rows' reference scores follow the largest seen score at a distance of at most kAttendSlack, in which exp2 still fits either type
-      constexpr float kAttendSlack = 8.0f;
-      float mx[NQ];
-      bool need = false;
 #pragma unroll
-      for (int qb = 0; qb < NQ; ++qb) {
-        mx[qb] = -INFINITY;
+        for (int db = 0; db < DB; ++db) any |= fp8_nans(vr[kb][db].x) | fp8_nans(vr[kb][db].y) | fp8_nans(vr[kb][db].z) | fp8_nans(vr[kb][db].w);
+        if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
+          int vis[NQ];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+          for (int qb = 0; qb < NQ; ++qb) {
+            vis[qb] = seen[qb] - t * kTile - 4 * g;
+            asm volatile("" : "+v"(vis[qb]));      // (its compares are made here, not kept in registers from the ones above)
+          }
 #pragma unroll
-          for (int e = 0; e < 16; ++e) mx[qb] = fmaxf(mx[qb], s[kb][qb][e]);
-        mx[qb] *= p.score_mul;
-        need |= mx[qb] > mref[qb] + kAttendSlack;
+          for (int db = 0; db < DB; ++db) attend8_nans<NQ>(vr[kb][db], kb, oacc[db], vis);
+        }
       }
-      if (__builtin_amdgcn_ballot_w64(need) != 0) {
+      uint32_t pk[NQ][8];
+      if constexpr (SOFTMAX) {
+        // the rows' reference scores follow the largest seen score at a distance of at most kAttendSlack, in which exp2 still fits either type
+        constexpr float kAttendSlack = 8.0f;
+        float mx[NQ];
+        bool need = false;
 #pragma unroll
         for (int qb = 0; qb < NQ; ++qb) {
-          const float mn = fmaxf(mref[qb], fmaxf(mx[qb], __shfl_xor(mx[qb], 32, 64)));
-          const float c = mn == mref[qb] ? 1.0f : __builtin_amdgcn_exp2f(mref[qb] - mn);     // from -inf: 0
-          mref[qb] = mn;
-          lsum[qb] *= c;
+          mx[qb] = -INFINITY;
 #pragma unroll
-          for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) oacc[db][qb][e] *= c;
+          for (int e = 0; e < 16; ++e) mx[qb] = fmaxf(mx[qb], s[qb][e]);
+          mx[qb] *= p.score_mul;
+          need |= mx[qb] > mref[qb] + kAttendSlack;
         }
-      }
+        if (__builtin_amdgcn_ballot_w64(need) != 0) {
 #pragma unroll
-      for (int qb = 0; qb < NQ; ++qb) {
-        const float m = mref[qb] == -INFINITY ? 0.f : mref[qb];      // (a row that has seen nothing: weights exp2(-inf) = 0)
+          for (int qb = 0; qb < NQ; ++qb) {
+            const float mn = fmaxf(mref[qb], fmaxf(mx[qb], __shfl_xor(mx[qb], 32, 64)));
+            const float c = mn == mref[qb] ? 1.0f : __builtin_amdgcn_exp2f(mref[qb] - mn);     // from -inf: 0
+            mref[qb] = mn;
+            lsum[qb] *= c;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) oacc[db][qb][e] *= c;
+          }
+        }
+#pragma unroll
+        for (int qb = 0; qb < NQ; ++qb) {
+          const float m = mref[qb] == -INFINITY ? 0.f : mref[qb];      // (a row that has seen nothing: weights exp2(-inf) = 0)
 #pragma unroll
           for (int e = 0; e < 16; e += 2) {
-            const float a = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][e], p.score_mul, -m)), b = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][e + 1], p.score_mul, -m));
+            const float a = __builtin_amdgcn_exp2f(fmaf(s[qb][e], p.score_mul, -m)), b = __builtin_amdgcn_exp2f(fmaf(s[qb][e + 1], p.score_mul, -m));
             lsum[qb] += a + b;
-            pk[kb][qb][e >> 1] = H::pack2(a, b);
+            pk[qb][e >> 1] = H::pack2(a, b);
           }
-      }
-    } else {
+        }
+      } else {
 #pragma unroll
-      for (int qb = 0; qb < NQ; ++qb)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int qb = 0; qb < NQ; ++qb)
 #pragma unroll
           for (int e = 0; e < 16; e += 2) {     // SiLU(s) / ln 2 with t = alpha s log2(e)
-            const float ta = s[kb][qb][e] * p.score_mul, tb = s[kb][qb][e + 1] * p.score_mul;
-            pk[kb][qb][e >> 1] = H::pack2(ta * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-ta)), tb * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-tb)));
+            const float ta = s[qb][e] * p.score_mul, tb = s[qb][e + 1] * p.score_mul;
+            pk[qb][e >> 1] = H::pack2(ta * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-ta)), tb * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-tb)));
           }
-    }
-    if (masked) {
-      uint32_t any = 0;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) any |= fp8_nans(vr[db][kb].x) | fp8_nans(vr[db][kb].y) | fp8_nans(vr[db][kb].z) | fp8_nans(vr[db][kb].w);
-      if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
-        int vis[NQ];
-#pragma unroll
-        for (int qb = 0; qb < NQ; ++qb) {
-          vis[qb] = seen[qb] - t * kTile - 4 * g;
-          asm volatile("" : "+v"(vis[qb]));      // (its compares are made here, not kept in registers from the ones above)
-        }
-        attend8_nans<NQ, DB>(vr, oacc, vis);
       }
-    }
-    // second product
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-          const u32x4_t vf = m == 0 ? fp8_frag<H>(vr[db][kb].x, vr[db][kb].y, sc.y) : fp8_frag<H>(vr[db][kb].z, vr[db][kb].w, sc.y);
+          const u32x4_t vf = m == 0 ? fp8_frag<H>(vr[kb][db].x, vr[kb][db].y, sc.y) : fp8_frag<H>(vr[kb][db].z, vr[kb][db].w, sc.y);
 #pragma unroll
           for (int qb = 0; qb < NQ; ++qb)
-            oacc[db][qb] = H::mfma(vf, make_uint4(pk[kb][qb][4 * m], pk[kb][qb][4 * m + 1], pk[kb][qb][4 * m + 2], pk[kb][qb][4 * m + 3]), oacc[db][qb]);
+            oacc[db][qb] = H::mfma(vf, make_uint4(pk[qb][4 * m], pk[qb][4 * m + 1], pk[qb][4 * m + 2], pk[qb][4 * m + 3]), oacc[db][qb]);
         }
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int kp = 0; kp < KP; ++kp) kr[kb][kp] = kn[kb][kp];
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) vr[db][kb] = vn[db][kb];
+      if constexpr (MORE) load_v(tn, kb);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     sc = sn;
+  };
+  int t = t0 + wave;
+  if (t < t1) {
+    sc = load_scales(t);
+    load_k(t, 0);
+    load_v(t, 0);
+    load_k(t, 1);
+    load_v(t, 1);
+    for (; t + kAttendWaves < t1; t += kAttendWaves) tile(std::true_type(), t);
+    tile(std::false_type(), t);
   }
 
   // the wavefronts' sums: upper half to lower half, twice (a fixed order)
@@ -312,73 +374,69 @@ __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend8_kernel(AttendPar
     }
     __syncthreads();
   }
-  if (wave != 0) return;
+  if (wave == 0) attend8_store<H, DH, NQ, SOFTMAX>(p, it, 0, lane, seen, oacc, mref, lsum);
+}
 
-  // element e of oacc[db][qb]: feature db*32 + 8*(e/4) + 4*g + e%4, row l32 of block qb
+// Adds the pieces of rows that were cut along the keys, in their order, and writes the rows.  One wavefront for 256 features of a row (four to a lane); the
+// pieces are loaded eight at a time.
+struct JoinUser {
+  int32_t row0, rows, keys, part0, parts;
+  int32_t cut0;        // rows of the launch's users before it
+};
+template <int USERS> struct JoinParams {
+  uint16_t* out;
+  int64_t out_stride;
+  const float *part, *ml;
+  int32_t n_users, n_rows, d, n_heads, causal;
+  JoinUser users[USERS];
+};
+template <typename H, bool SOFTMAX, int USERS>
+__global__ __launch_bounds__(256) void attend8_join_kernel(JoinParams<USERS> p) {
+  const int lane = threadIdx.x & 63, segs_sh = max(__builtin_ctz(p.d) - 8, 0);
+  const int unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  const int row = unit >> segs_sh, f = (unit - (row << segs_sh)) * 256 + lane * 4;
+  if (row >= p.n_rows) return;
+  int at = -1;
 #pragma unroll
-  for (int qb = 0; qb < NQ; ++qb) {
-    const int r = qb * 32 + l32;
-    if constexpr (SOFTMAX) lsum[qb] += __shfl_xor(lsum[qb], 32, 64);
-    if (r >= n_rows) continue;
-    if (u.parts == 1) {
-      const float mul = seen[qb] == 0 ? 0.f : SOFTMAX ? 1.0f / lsum[qb] : 0.69314718055994531f / (float)seen[qb];
-      uint16_t* dst = p.out + (int64_t)(u.row0 + first_row + r) * p.out_stride + head * DH + 4 * g;
+  for (int u0 = 0; u0 < USERS; u0 += 64) {
+    const bool there = u0 + lane < p.n_users;
+    at += __builtin_popcountll(__builtin_amdgcn_ballot_w64(there && p.users[there ? u0 + lane : 0].cut0 <= row));
+  }
+  const JoinUser u = p.users[__builtin_amdgcn_readfirstlane(at)];
+  const int r = row - u.cut0, seen = p.causal ? max(u.keys - u.rows + 1 + r, 0) : u.keys;
+  const bool mine = f < p.d;           // (d = 128: half of the lanes)
+  const int head = (mine ? f : 0) / (p.d / p.n_heads);
+  const float* x = p.part + ((int64_t)u.part0 + r) * p.d + (mine ? f : 0);
+  const int64_t step = (int64_t)u.rows * p.d;      // between a row's pieces
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float M = -INFINITY, l = 0.f;
+  for (int k0 = 0; k0 < u.parts; k0 += 8) {
+    float4 v[8];
+    float2 ml[8];
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
+    for (int k = 0; k < 8; ++k) {
+      const int kk = min(k0 + k, u.parts - 1);
+      v[k] = *reinterpret_cast<const float4*>(x + kk * step);
+      if constexpr (SOFTMAX) ml[k] = *reinterpret_cast<const float2*>(p.ml + (((int64_t)u.part0 + (int64_t)kk * u.rows + r) * p.n_heads + head) * 2);
+    }
 #pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-          uint2 w = make_uint2(H::pack2(oacc[db][qb][4 * e4] * mul, oacc[db][qb][4 * e4 + 1] * mul), H::pack2(oacc[db][qb][4 * e4 + 2] * mul, oacc[db][qb][4 * e4 + 3] * mul));
-          if (seen[qb] == 0) w = make_uint2(0, 0);
-          *reinterpret_cast<uint2*>(dst + db * 32 + 8 * e4) = w;
-        }
-    } else {
-      const int64_t pr = (int64_t)u.part0 + (int64_t)piece * u.rows + first_row + r;
-      float* dst = p.part + pr * p.d + head * DH + 4 * g;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4)
-          *reinterpret_cast<float4*>(dst + db * 32 + 8 * e4) =
-              make_float4(oacc[db][qb][4 * e4], oacc[db][qb][4 * e4 + 1], oacc[db][qb][4 * e4 + 2], oacc[db][qb][4 * e4 + 3]);
+    for (int k = 0; k < 8; ++k) {
+      if (k0 + k >= u.parts) continue;
       if constexpr (SOFTMAX) {
-        if (g == 0) *reinterpret_cast<float2*>(p.ml + (pr * p.n_heads + head) * 2) = make_float2(mref[qb], lsum[qb]);
+        const float mn = fmaxf(M, ml[k].x), c0 = M == mn ? 1.0f : __builtin_amdgcn_exp2f(M - mn), c1 = ml[k].x == mn ? 1.0f : __builtin_amdgcn_exp2f(ml[k].x - mn);
+        o = make_float4(o.x * c0 + v[k].x * c1, o.y * c0 + v[k].y * c1, o.z * c0 + v[k].z * c1, o.w * c0 + v[k].w * c1);
+        l = l * c0 + ml[k].y * c1;
+        M = mn;
+      } else {
+        o = make_float4(o.x + v[k].x, o.y + v[k].y, o.z + v[k].z, o.w + v[k].w);
       }
     }
   }
-}
-
-// Adds the pieces of rows that were cut along the keys, in their order, and writes the rows.  One thread for four features of a row.
-template <typename H, bool SOFTMAX>
-__global__ __launch_bounds__(256) void attend8_join_kernel(AttendParams p, int n_rows, int row_base) {
-  const int lane = threadIdx.x & 63, per_row = p.d / 4;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int row = row_base + (int)(id / per_row), f = (int)(id % per_row) * 4, head = f / (p.d / p.n_heads);
-  if (row >= row_base + n_rows) return;
-  int at = 0;
-  for (int i = 1; i < p.n_users; ++i) at += p.users[i].row0 <= row ? 1 : 0;      // (users in the order of their rows)
-  (void)lane;
-  const AttendUser& u = p.users[at];
-  if (u.parts <= 1 || row - u.row0 >= u.rows) return;
-  const int seen = attend_seen(u, row - u.row0, p.causal);
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  float M = -INFINITY, l = 0.f;
-  for (int k = 0; k < u.parts; ++k) {
-    const int64_t pr = (int64_t)u.part0 + (int64_t)k * u.rows + (row - u.row0);
-    const float4 x = *reinterpret_cast<const float4*>(p.part + pr * p.d + f);
-    if constexpr (SOFTMAX) {
-      const float2 ml = *reinterpret_cast<const float2*>(p.ml + (pr * p.n_heads + head) * 2);
-      const float mn = fmaxf(M, ml.x), c0 = M == mn ? 1.0f : __builtin_amdgcn_exp2f(M - mn), c1 = ml.x == mn ? 1.0f : __builtin_amdgcn_exp2f(ml.x - mn);
-      o = make_float4(o.x * c0 + x.x * c1, o.y * c0 + x.y * c1, o.z * c0 + x.z * c1, o.w * c0 + x.w * c1);
-      l = l * c0 + ml.y * c1;
-      M = mn;
-    } else {
-      o = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
-    }
-  }
+  if (!mine) return;
   const float mul = SOFTMAX ? 1.0f / l : 0.69314718055994531f / (float)seen;
   uint2 w = make_uint2(H::pack2(o.x * mul, o.y * mul), H::pack2(o.z * mul, o.w * mul));
   if (seen == 0) w = make_uint2(0, 0);
-  *reinterpret_cast<uint2*>(p.out + (int64_t)row * p.out_stride + f) = w;
+  *reinterpret_cast<uint2*>(p.out + (int64_t)(u.row0 + r) * p.out_stride + f) = w;
 }
 
 }  // namespace relaygr

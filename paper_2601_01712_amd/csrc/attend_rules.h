@@ -1,0 +1,67 @@
+// Which kernel a launch of attention over the 8-bit cache takes and how its key sequences are cut, by the batch's sizes.  No HIP in this file: the
+// tests compile it with the host compiler, so that a test of a kernel can say that its launches take that kernel.
+#pragma once
+
+#include <stdint.h>
+
+#include <algorithm>
+#include <vector>
+
+#include "plan.h"
+
+namespace relaygr {
+
+struct AttendLen { int rows, keys; };      // of a user: query rows, tokens that take part
+struct AttendRule {
+  int blocks = 1;        // 32-row blocks of an item
+  bool once = false;     // the kernel whose loads are not kept in the caches
+  int piece = 0;         // key tiles of a piece, about (0: nothing is cut)
+};
+
+// Pieces of a key sequence of nk tiles: as many as it has of `piece` tiles, to nearest, none of them empty.
+constexpr int kAttendParts = 64;
+inline int attend_parts(int nk, int piece) {
+  if (piece <= 0 || nk == 0) return 1;
+  const int parts = std::max(1, std::min((nk + piece / 2) / piece, kAttendParts)), per = (nk + parts - 1) / parts;
+  return (nk + per - 1) / per;
+}
+
+// A workgroup is four wavefronts that share an item's key tiles, and two or three of them a compute unit are full speed.
+//
+// Two blocks of 32 rows an item (one conversion of the codes for twice the rows) where the launch still has four items a compute unit and users have
+// so many rows that few blocks are empty; at d_head 64, where the registers hold them.  us, one block / two, d = 512: 16 users of 512 rows over 4096
+// keys 94.4 / 88.1, 32 of 200 to 1000 over about 4096 249 / 238; fewer items: one of 512 over 4096 13.4 / 15.4; few rows: 64 of 50 to 100 103 / 120; d_head 32, 16
+// of 500 to 1000 over 8000 211 / 218.
+//
+// Sequences are cut where the launch has fewer items than the chip has compute units (at d = 512 one user of 4096 keys: 512 rows, 128 items, uncut 16.1, 256
+// pieces 13.4, 512 14.8; one row of 16 384 keys, 8 items, uncut 50, 128 pieces 10.4, 256 11.2, 512 14.4), and where items are of unequal length
+// those that would be left running behind the others (32 users of 8 to 60 rows over about 4096 keys, 48 key tiles a piece 40.6, uncut 55.6): each cut
+// is a partial sum to write and read and the first one a launch.  448 equal items of 33 tiles: uncut 12.3, in halves 14.5.
+//
+// Codes that one item alone reads, more of them than the caches could keep until they are read again: 128 users of 8192 keys, one row each (1.07 GB) 180 / 162
+// without keeping, of 2048 and four rows (268 MB) 51.3 / 44.8; 64 of 4096 and 20 at d = 1024 93.7 / 83.4.
+constexpr int kLeastPiece = 4;
+constexpr int64_t kOnceBytes = (int64_t)128 << 20;      // half of the last-level cache
+inline AttendRule attend_rule(const std::vector<AttendLen>& users, int heads, int dh, int n_cus) {
+  AttendRule r;
+  int64_t rows = 0, keys = 0, items1 = 0, items2 = 0, key_tiles = 0, most = 0;
+  int most_rows = 0;
+  for (const AttendLen& u : users) {
+    const int64_t nk = (u.keys + kTile - 1) / kTile;
+    rows += u.rows; keys += u.keys;
+    items1 += (u.rows + 31) / 32; items2 += (u.rows + 63) / 64;
+    most_rows = std::max(most_rows, u.rows);
+    most = std::max(most, nk);
+  }
+  if (dh == 64 && items2 * heads >= 4 * n_cus && rows >= 192 * (int64_t)users.size()) r.blocks = 2;
+  r.once = most_rows <= 32 && 2 * keys * heads * dh >= kOnceBytes;
+  const int64_t items = (r.blocks == 2 ? items2 : items1) * heads;
+  for (const AttendLen& u : users) key_tiles += (u.rows + 32 * r.blocks - 1) / (32 * r.blocks) * (int64_t)((u.keys + kTile - 1) / kTile) * heads;
+  const bool equal = 3 * most * items <= 4 * key_tiles;                   // the longest is at most a third over the mean
+  if (equal && items >= n_cus) return r;
+  const int64_t slots = equal ? n_cus : 2 * n_cus;
+  r.piece = (int)std::max<int64_t>(kLeastPiece, std::min<int64_t>((key_tiles + slots - 1) / slots, 1 << 20));
+  return r;
+}
+
+}  // namespace relaygr

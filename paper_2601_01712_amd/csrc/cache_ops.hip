@@ -7,6 +7,7 @@
 #include <vector>
 
 #include "attend8.h"
+#include "attend_rules.h"
 #include "errors.h"
 #include "kv8.h"
 
@@ -120,22 +121,17 @@ int move_rows(const char* what, KvPool* pool, int32_t layer, const relaygr_kv_ro
   return launch_rows<WRITE, kRowUsers>(what, pool, layer, r, entries, k, k_stride, v, v_stride, st);
 }
 
-template <typename H, bool SM>
-void launch_attend(const AttendParams& p, int dh, bool wide, int rows, int row_base, bool cut, hipStream_t st) {
+template <typename H, int DH, bool SM, int USERS>
+void launch_attend(const AttendParams<USERS>& p, int blocks, bool once, hipStream_t st) {
   const int nh = p.n_heads;
   const dim3 grid(nh >= 8 ? p.n_items * nh : (p.n_items + 8 / nh - 1) / (8 / nh) * 8), block(kAttendWaves * 64);
-  switch (dh) {
-    case 32:
-      if (wide) hipLaunchKernelGGL((attend8_kernel<H, 32, 2, SM>), grid, block, 0, st, p);
-      else hipLaunchKernelGGL((attend8_kernel<H, 32, 1, SM>), grid, block, 0, st, p);
-      break;
-    case 64:
-      if (wide) hipLaunchKernelGGL((attend8_kernel<H, 64, 2, SM>), grid, block, 0, st, p);
-      else hipLaunchKernelGGL((attend8_kernel<H, 64, 1, SM>), grid, block, 0, st, p);
-      break;
-    default: hipLaunchKernelGGL((attend8_kernel<H, 128, 1, SM>), grid, block, 0, st, p); break;
+  if constexpr (USERS > kFewAttendUsers) {
+    if constexpr (DH == 64) {
+      if (blocks == 2) { hipLaunchKernelGGL((attend8_kernel<H, DH, 2, SM, false, USERS>), grid, block, 0, st, p); return; }
+    }
+    if (once) { hipLaunchKernelGGL((attend8_kernel<H, DH, 1, SM, true, USERS>), grid, block, 0, st, p); return; }
   }
-  if (cut) hipLaunchKernelGGL((attend8_join_kernel<H, SM>), dim3((unsigned)(((int64_t)rows * (p.d / 4) + 255) / 256)), dim3(256), 0, st, p, rows, row_base);
+  hipLaunchKernelGGL((attend8_kernel<H, DH, 1, SM, false, USERS>), grid, block, 0, st, p);
 }
 
 }  // namespace
@@ -167,79 +163,81 @@ int relaygr::attend8(KvPool* pool, const AttendCall& c, hipStream_t st) {
   if (rc != RELAYGR_OK || r->n_users == 0) return rc;
   const relaygr_model_config& cfg = pool->cfg;
   const int d = cfg.d_model, H = cfg.n_heads, dh = d / H;
-  struct Work { int user, rows, keys; };
+  struct Work { int user, rows, keys, parts, per; };
   std::vector<Work> work;
-  int64_t rows_all = 0;
-  int most_rows = 0;
+  std::vector<AttendLen> lens;
   for (int u = 0; u < r->n_users; ++u) {
     const int keys = r->key_len ? r->key_len[u] : entries[u].prefix_len, n = r->row_off[u + 1] - r->row_off[u];
     if (keys < 0 || keys > entries[u].prefix_len) return fail(RELAYGR_EINVAL, "%s: user %d: %d keys of an entry of %d tokens", what, u, keys, entries[u].prefix_len);
     if (n == 0) continue;
-    work.push_back({u, n, keys});
-    rows_all += n;
-    most_rows = std::max(most_rows, n);
+    work.push_back({u, n, keys, 1, 0});
+    lens.push_back({n, keys});
   }
   if (work.empty()) return RELAYGR_OK;
   if ((rc = check_rows_array(what, "q", c.q, c.q_stride, d)) != RELAYGR_OK) return rc;
   if ((rc = check_rows_array(what, "out", c.out, c.out_stride, d)) != RELAYGR_OK) return rc;
 
-  const bool wide = dh <= 64 && most_rows > 32;
-  const int item_rows = wide ? 64 : 32;
-  // pieces of the key sequences
-  const int64_t slots = 2 * c.n_cus;
-  int64_t items = 0, tiles = 0;
-  for (const Work& w : work) {
-    const int64_t rt = (w.rows + item_rows - 1) / item_rows;
-    items += rt * H;
-    tiles += rt * H * ((w.keys + kTile - 1) / kTile);
-  }
-  int64_t per = std::max<int64_t>(kAttendWaves, (tiles + slots - 1) / slots);
-  if (items >= 2 * slots || !c.scratch) per = 1 << 30;
+  AttendRule rule = attend_rule(lens, H, dh, c.n_cus);
+  if (!c.scratch) rule.piece = 0;
+  const int blocks = rule.blocks, item_rows = 32 * blocks;
+  const bool once = rule.once;
   const size_t row_bytes = (size_t)d * 4 + (c.softmax ? (size_t)H * 8 : 0);
-  auto parts_of = [&](const Work& w) { const int64_t nk = (w.keys + kTile - 1) / kTile; return (int)std::max<int64_t>(1, (nk + per - 1) / per); };
   int64_t partial_rows;
-  for (;; per *= 2) {
+  for (;; rule.piece = rule.piece > 1 << 20 ? 0 : 2 * rule.piece) {      // (0: nothing is cut)
     partial_rows = 0;
-    for (const Work& w : work) { const int parts = parts_of(w); if (parts > 1) partial_rows += (int64_t)parts * w.rows; }
+    for (Work& w : work) {
+      const int nk = (w.keys + kTile - 1) / kTile;
+      w.parts = attend_parts(nk, rule.piece);
+      w.per = std::max(1, (nk + w.parts - 1) / w.parts);
+      if (w.parts > 1) partial_rows += (int64_t)w.parts * w.rows;
+    }
     if (partial_rows == 0 || ((size_t)partial_rows * row_bytes <= c.scratch_bytes && partial_rows < (1ll << 31))) break;
   }
+  std::stable_sort(work.begin(), work.end(), [](const Work& a, const Work& b) { return a.per > b.per; });    // the longest pieces first
 
   (void)hipGetLastError();
-  AttendParams p = {};
-  p.q = (const uint16_t*)c.q; p.out = (uint16_t*)c.out; p.q_stride = c.q_stride; p.out_stride = c.out_stride;
-  p.tile_stride = pool->tile_stride;
-  p.scales_off = q8_scales_off(cfg, c.layer) - c.layer * pool->layer_stride;
-  p.part = (float*)c.scratch;
-  p.ml = (float*)(c.scratch + (size_t)partial_rows * d * 4);
-  p.d = d; p.n_heads = H; p.causal = c.causal ? 1 : 0;
-  p.score_mul = 1.4426950408889634f / sqrtf((float)dh);
+  float *part = (float*)c.scratch, *ml = (float*)(c.scratch + (size_t)partial_rows * d * 4);
   int32_t part0 = 0;
-  for (size_t i = 0; i < work.size();) {
-    p.n_users = 0; p.n_items = 0;
-    bool cut = false;
-    const int row_base = r->row_off[work[i].user];
-    int row_end = row_base;
-    for (; i < work.size() && p.n_users < kAttendUsers; ++i) {
-      const Work& w = work[i];
-      const int parts = parts_of(w), nk = (w.keys + kTile - 1) / kTile;
-      AttendUser& u = p.users[p.n_users++];
-      u.kv = entry_tile0(pool, entries[w.user]) + c.layer * pool->layer_stride;
-      u.row0 = r->row_off[w.user]; u.rows = w.rows; u.keys = w.keys;
-      u.item0 = p.n_items; u.part0 = part0; u.parts = parts; u.per = std::max(1, (nk + parts - 1) / parts); u.pad_ = 0;
-      p.n_items += (w.rows + item_rows - 1) / item_rows * parts;
-      if (parts > 1) { part0 += parts * w.rows; cut = true; }
-      row_end = u.row0 + w.rows;
+  auto launch = [&](auto users) -> int {
+    constexpr int USERS = decltype(users)::value;
+    AttendParams<USERS> p = {};
+    JoinParams<USERS> j = {};
+    p.q = (const uint16_t*)c.q; p.out = (uint16_t*)c.out; p.q_stride = c.q_stride; p.out_stride = c.out_stride;
+    p.slab = (const char*)pool->slab + c.layer * pool->layer_stride;
+    p.page_bytes = (int64_t)pool->page_bytes; p.tile_stride = pool->tile_stride;
+    p.scales_off = q8_scales_off(cfg, c.layer) - c.layer * pool->layer_stride;
+    p.part = part; p.ml = ml;
+    p.d = d; p.n_heads = H; p.causal = c.causal ? 1 : 0;
+    p.score_mul = 1.4426950408889634f / sqrtf((float)dh);
+    j.out = p.out; j.out_stride = p.out_stride; j.part = part; j.ml = ml; j.d = d; j.n_heads = H; j.causal = p.causal;
+    for (size_t i = 0; i < work.size();) {
+      p.n_users = 0; p.n_items = 0; j.n_users = 0; j.n_rows = 0;
+      for (; i < work.size() && p.n_users < USERS; ++i) {
+        const Work& w = work[i];
+        const int32_t row0 = r->row_off[w.user];
+        p.users[p.n_users++] = {(int32_t)entries[w.user].page0, row0, w.rows, w.keys, p.n_items, part0, (uint32_t)w.parts | (uint32_t)w.per << 7};
+        p.n_items += (w.rows + item_rows - 1) / item_rows * w.parts;
+        if (w.parts == 1) continue;
+        j.users[j.n_users++] = {row0, w.rows, w.keys, part0, w.parts, j.n_rows};
+        j.n_rows += w.rows;
+        part0 += w.parts * w.rows;
+      }
+      by_head(cfg, [&](auto h, auto dim) {
+        using HT = decltype(h);
+        constexpr int DH = decltype(dim)::value;
+        if (c.softmax) launch_attend<HT, DH, true>(p, blocks, once, st);
+        else launch_attend<HT, DH, false>(p, blocks, once, st);
+        if (j.n_users == 0) return;
+        const dim3 grid((unsigned)(((int64_t)j.n_rows * std::max(1, d / 256) + 3) / 4));
+        if (c.softmax) hipLaunchKernelGGL((attend8_join_kernel<HT, true, USERS>), grid, dim3(256), 0, st, j);
+        else hipLaunchKernelGGL((attend8_join_kernel<HT, false, USERS>), grid, dim3(256), 0, st, j);
+      });
+      LAUNCH_CHECK(what);
     }
-    auto go = [&](auto h) {
-      using HT = decltype(h);
-      if (c.softmax) launch_attend<HT, true>(p, dh, wide, row_end - row_base, row_base, cut, st);
-      else launch_attend<HT, false>(p, dh, wide, row_end - row_base, row_base, cut, st);
-    };
-    if (cfg.dtype == RELAYGR_DTYPE_FP16) go(F16());
-    else go(Bf16());
-    LAUNCH_CHECK(what);
-  }
-  return RELAYGR_OK;
+    return RELAYGR_OK;
+  };
+  if ((int)work.size() <= kFewAttendUsers && blocks == 1 && !once) return launch(std::integral_constant<int, kFewAttendUsers>());
+  return launch(std::integral_constant<int, kAttendUsers>());
 }
 
 // (the planning allocates host memory: running out of it is an error code of the call)

@@ -1,5 +1,13 @@
 """The 8-bit K/V cache in 64 bits, from its definition (numpy; shares no code with the library), and what the GPU tests of it need."""
+import ctypes as C
+import functools
+import os
+import shutil
+import subprocess
+import tempfile
+
 import numpy as np
+import pytest
 import torch
 
 import paper_2601_01712_amd as rg
@@ -120,3 +128,23 @@ def context_for(model, users, rows):
 
 def model(d, heads, dtype, form="silu", layers=2):
     return synth.ModelConfig(layers, d, heads, dtype, attention=form)
+
+
+@functools.lru_cache(maxsize=None)
+def rule_shim():
+    if shutil.which("g++") is None:
+        pytest.skip("no g++")
+    with tempfile.TemporaryDirectory() as tmp:
+        lib = os.path.join(tmp, "attend_rule.so")
+        src = os.path.join(os.path.dirname(os.path.abspath(__file__)), "attend_rule_shim.cpp")
+        subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-Wextra", "-Werror", "-shared", "-fPIC", src, "-o", lib], check=True)
+        return C.CDLL(lib)
+
+
+def attend_rule(rows, keys, heads, dh, n_cus=256):
+    """What a launch of attention takes: 32-row blocks of an item, whether codes are loaded once, key tiles of a piece, most pieces of a user."""
+    both = [(m, n) for m, n in zip(rows, keys) if m > 0]
+    r, k = (np.array(x, np.int32) for x in zip(*both))
+    out = np.zeros(4, np.int32)
+    rule_shim().attend_rule_of(len(both), r.ctypes.data_as(C.c_void_p), k.ctypes.data_as(C.c_void_p), heads, dh, n_cus, out.ctypes.data_as(C.c_void_p))
+    return dict(zip(("blocks", "once", "piece", "parts"), out.tolist()))

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2601_01712_amd as rg
-from q8_util import TORCH, attend, context_for, held, model, offsets, pool_for, seen_by_rows, values
+from q8_util import TORCH, attend, attend_rule, context_for, held, model, offsets, pool_for, seen_by_rows, values
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -13,7 +13,7 @@ DEV = "cuda:0"
 class Case:
     """Entries of the given lengths in layer 1 of 2, their cached values in 64 bits, and a context."""
 
-    def __init__(self, d, heads, dtype, form, lens, rows, seed=0, spread=0.6):
+    def __init__(self, d, heads, dtype, form, lens, rows, seed=0, spread=0.6, check=None):
         self.d, self.heads, self.dtype, self.form, self.lens, self.rows = d, heads, dtype, form, lens, rows
         m = model(d, heads, dtype, form)
         self.rng = np.random.default_rng(seed)
@@ -22,7 +22,8 @@ class Case:
         (k, k64), (v, v64) = (values(self.rng, sum(lens), d, dtype, spread) for _ in range(2))
         rg.relaygr_kv_pool_write(self.pool, 1, rg.KvRows(self.handles, offsets(lens)), k.to(DEV), v.to(DEV))
         at = offsets(lens)
-        self.k, self.v = ([held(x[at[u]:at[u + 1]].reshape(n, heads, d // heads), dtype) for u, n in enumerate(lens)] for x in (k64, v64))
+        self.checked = range(len(lens)) if check is None else check
+        self.k, self.v = ([None if u not in self.checked else held(x[at[u]:at[u + 1]].reshape(n, heads, d // heads), dtype) for u, n in enumerate(lens)] for x in (k64, v64))
         self.q, self.q64 = values(self.rng, sum(rows), d, dtype, spread)
         self.q = self.q.to(DEV)
 
@@ -96,6 +97,31 @@ def test_many_users_more_than_a_launch_takes():
     c = Case(128, 2, "bf16", "softmax", lens, rows, seed=29)
     c.check(c.run())
     c.check(c.run(causal=True), causal=True)
+
+
+#   users, rows, keys, d, heads, and what the launch takes: blocks, once, whether it is cut
+KERNELS = [
+    (33, 200, 70, 512, 8, 2, 0, False),
+    (33, 250, [64] * 30 + [700] * 3, 512, 8, 2, 0, True),
+    (80, 3, 2100, 512, 8, 1, 1, False),
+    (20, 5, [200] * 19 + [9000], 256, 4, 1, 0, True),
+    (65, 7, [1100] * 64 + [17000], 1024, 8, 1, 1, True),
+]
+
+
+@pytest.mark.parametrize("form", ["silu", "softmax"])
+@pytest.mark.parametrize("case", range(len(KERNELS)))
+def test_the_kernels_of_large_launches(case, form):
+    """Items of two row blocks, codes loaded once, launches of many users whose rows are joined: some of the users against the formula."""
+    users, m, n, d, heads, blocks, once, cut = KERNELS[case]
+    lens = n if isinstance(n, list) else [n] * users
+    rows = [m - u % 3 for u in range(users)]
+    rule = attend_rule(rows, lens, heads, d // heads)
+    assert (rule["blocks"], rule["once"], rule["parts"] > 1) == (blocks, once, cut)
+    c = Case(d, heads, "bf16", form, lens, rows, seed=61 + case, check=(0, users // 2, users - 1))
+    c.check(c.run(), users=c.checked)
+    if blocks == 2:
+        c.check(c.run(causal=True), causal=True, users=c.checked)
 
 
 def test_large_scores():

@@ -8,7 +8,7 @@ import torch
 
 import paper_2601_01712_amd as rg
 from paper_2601_01712_amd import binding as B
-from q8_util import e4m3, exponent, held
+from q8_util import attend_rule, e4m3, exponent, held, rule_shim
 
 CFG = dict(n_layers=3, d_model=256, n_heads=4, dtype="bf16")
 
@@ -168,3 +168,29 @@ def test_the_reference_of_the_gpu_tests():
     assert exponent(np.zeros(3)) == -100 and exponent(np.array([np.nan, np.inf])) == -100
     y = held(np.array([1.0, -3.1, np.inf, np.nan, 1e-4]).reshape(5, 1, 1), "bf16").ravel()
     assert y[0] == 1.0 and y[1] == -3.0 and np.isnan(y[2:4]).all() and y[4] == 7 * 2.0 ** -16
+
+
+def test_pieces_of_a_key_sequence():
+    """Every key tile is in one piece, none is empty, and there are at most 64 of them."""
+    for nk in list(range(0, 70)) + [127, 128, 129, 255, 256, 1000, 33554431]:
+        for piece in (0, 1, 3, 4, 8, 100, 1 << 20):
+            parts = rule_shim().attend_parts_of(nk, piece)
+            per = max(1, -(-nk // parts))
+            assert 1 <= parts <= 64 and (nk == 0 or (parts - 1) * per < nk <= parts * per)
+            assert piece > 0 or parts == 1
+    assert rule_shim().attend_parts_of(5, 4) == 1 and rule_shim().attend_parts_of(6, 4) == 2
+
+
+def test_rule_of_the_attention_kernels():
+    def rule(users, rows, keys, heads=8, dh=64):
+        return attend_rule([rows] * users, [keys] * users, heads, dh)
+    assert rule(16, 512, 4096) == {"blocks": 2, "once": 0, "piece": 0, "parts": 1}
+    assert rule(16, 512, 4096, dh=128)["blocks"] == 1 and rule(16, 512, 4096, dh=32)["blocks"] == 1
+    assert rule(64, 100, 4096)["blocks"] == 1 and rule(1, 512, 4096)["blocks"] == 1
+    assert rule(128, 1, 8192)["once"] == 1 and rule(128, 33, 8192)["once"] == 0 and rule(8, 1, 8192)["once"] == 0
+    assert rule(1, 1, 2048, heads=4)["parts"] == 8                       # four items: cut until the pieces are short
+    assert rule(1, 512, 4096)["parts"] == 2                              # 128 items: one for each compute unit and no more
+    assert rule(20, 20, 300)["parts"] == 1                               # too short to be worth a second launch
+    long_one = attend_rule([30] * 32, [1000] * 31 + [16384], 8, 64)
+    assert long_one["parts"] > 4 and attend_rule([30] * 32, [1000] * 32, 8, 64)["parts"] == 1
+    assert attend_rule([5], [0], 8, 64)["parts"] == 1
