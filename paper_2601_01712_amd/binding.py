@@ -426,8 +426,13 @@ class _KvCall:
             self.guard.__exit__(*exc)
 
 
-def _new_rows(pool: KvPool, rows: KvRows) -> torch.Tensor:
-    return torch.empty((rows.n_rows, pool.cfg.d_model), dtype=_torch_dtype(pool.dtype), device=pool.slab.device)
+def _result_rows(what: str, pool: KvPool, rows: KvRows, t: Optional[torch.Tensor]):
+    """A result's tensor (made here if the caller gives none), its address and the elements between its rows."""
+    if t is not None:
+        return (t, *_kv_rows_array(what, pool, rows, t))
+    d = pool.cfg.d_model
+    t = torch.empty((rows.n_rows, d), dtype=_torch_dtype(pool.dtype), device=pool.slab.device)
+    return t, (t.data_ptr() if rows.n_rows else None), d
 
 
 def relaygr_kv_pool_write(pool: KvPool, layer: int, rows: KvRows, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
@@ -442,10 +447,8 @@ def relaygr_kv_pool_read(pool: KvPool, layer: int, rows: KvRows, k: Optional[tor
                          stream=None):
     """(k, v): the values that tokens of the entries stand for, [rows, d_model] each (made here if not given)."""
     with _KvCall(pool, stream) as st:
-        k = _new_rows(pool, rows) if k is None else k
-        v = _new_rows(pool, rows) if v is None else v
-        kp, ks = _kv_rows_array("kv_pool_read: k", pool, rows, k)
-        vp, vs = _kv_rows_array("kv_pool_read: v", pool, rows, v)
+        k, kp, ks = _result_rows("kv_pool_read: k", pool, rows, k)
+        v, vp, vs = _result_rows("kv_pool_read: v", pool, rows, v)
         _check(load_library().relaygr_kv_pool_read(pool.handle, layer, rows.ref, kp, ks, vp, vs, st))
     return k, v
 
@@ -455,8 +458,7 @@ def relaygr_cache_attend(ctx: Context, pool: KvPool, layer: int, rows: KvRows, q
     """One layer's attention of query rows over entries of an 8-bit pool, in the context's form: [rows, d_model] (made here if not given)."""
     qp, qs = _kv_rows_array("cache_attend: q", pool, rows, q)
     with _KvCall(pool, stream) as st:
-        out = _new_rows(pool, rows) if out is None else out
-        op, os_ = _kv_rows_array("cache_attend: out", pool, rows, out)
+        out, op, os_ = _result_rows("cache_attend: out", pool, rows, out)
         _check(load_library().relaygr_cache_attend(ctx.handle, pool.handle, layer, rows.ref, int(causal), qp, qs, op, os_, st))
     return out
 

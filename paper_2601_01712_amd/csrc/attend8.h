@@ -35,6 +35,7 @@ template <int USERS> struct AttendParams {
   float* ml;                         // softmax form: [partial rows][n_heads][2] reference score (log2 units) and sum of weights
   int32_t n_users, n_items, d, n_heads, causal;
   float score_mul;                   // alpha * log2(e)
+  uint32_t* arrived;                 // few users: pieces of a (row tile, head) that are done, zero between launches; null: a launch of its own joins them
   AttendUser users[USERS];
 };
 // Tokens that row i of the user sees.
@@ -152,6 +153,77 @@ __device__ __forceinline__ void attend8_store(const AttendParams<USERS>& p, cons
       if constexpr (SOFTMAX) {
         if (g == 0) *reinterpret_cast<float2*>(p.ml + (pr * p.n_heads + it.head) * 2) = make_float2(mref[qb], lsum);
       }
+    }
+  }
+}
+
+// The sums of a row's pieces, four features to a lane.  Pieces are added in 256 / DH groups (piece k in group k mod groups), in their order, and then
+// the groups pairwise, lower to upper: one order, whichever of the two joins below a launch takes.
+template <bool SOFTMAX> struct PieceSum {
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float M = -INFINITY, l = 0.f;
+  __device__ __forceinline__ void add(const float4& x, float m, float w) {
+    if constexpr (SOFTMAX) {
+      const float mn = fmaxf(M, m), c0 = M == mn ? 1.0f : __builtin_amdgcn_exp2f(M - mn), c1 = m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+      o = make_float4(fmaf(x.x, c1, o.x * c0), fmaf(x.y, c1, o.y * c0), fmaf(x.z, c1, o.z * c0), fmaf(x.w, c1, o.w * c0));
+      l = fmaf(w, c1, l * c0);
+      M = mn;
+    } else {
+      o = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
+    }
+  }
+  template <typename H> __device__ __forceinline__ uint2 out(int seen) const {
+    const float mul = SOFTMAX ? 1.0f / l : 0.69314718055994531f / (float)seen;
+    return seen == 0 ? make_uint2(0, 0) : make_uint2(H::pack2(o.x * mul, o.y * mul), H::pack2(o.z * mul, o.w * mul));
+  }
+};
+
+// Joins the pieces of an item's rows in the workgroup that is the last of them to arrive: every workgroup of the item comes here once its partial sums are
+// stored by its wavefront 0.  Rows go to the wavefronts in turn, four at a time; a row's groups are side by side in a wavefront.
+template <typename H, int DH, bool SOFTMAX, int USERS>
+__device__ __forceinline__ void attend8_join_last(const AttendParams<USERS>& p, const AttendItem& it, int wave, int lane) {
+  constexpr int LANES = DH / 4, GROUPS = 64 / LANES;
+  __shared__ int last;
+  if (wave == 0) {
+    uint32_t* count = p.arrived + (it.u.item0 + it.first_row / 32) * p.n_heads + it.head;
+    if (lane == 0) {      // (the release is of all the wavefront's stores)
+      const uint32_t before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+      last = before + 1 == (uint32_t)it.u.parts();
+      if (last) *count = 0;
+    }
+  }
+  __syncthreads();
+  if (!last) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+  const int group = lane / LANES, f = it.head * DH + (lane % LANES) * 4, parts = it.u.parts();
+  const int64_t step = (int64_t)it.u.rows;
+  for (int r0 = wave; r0 < it.n_rows; r0 += 16) {
+    PieceSum<SOFTMAX> sum[4];
+    for (int k = group; k < parts + group; k += GROUPS) {      // (as many turns for every lane)
+      float4 x[4];
+      float2 ml[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t pr = it.u.part0 + min(k, parts - 1) * step + it.first_row + min(r0 + 4 * i, it.n_rows - 1);
+        x[i] = *reinterpret_cast<const float4*>(p.part + pr * p.d + f);
+        ml[i] = SOFTMAX ? *reinterpret_cast<const float2*>(p.ml + (pr * p.n_heads + it.head) * 2) : make_float2(0.f, 0.f);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (k < parts) sum[i].add(x[i], ml[i].x, ml[i].y);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int by = LANES; by < 64; by *= 2) {
+        PieceSum<SOFTMAX>& a = sum[i];
+        const float4 x = make_float4(__shfl_xor(a.o.x, by, 64), __shfl_xor(a.o.y, by, 64), __shfl_xor(a.o.z, by, 64), __shfl_xor(a.o.w, by, 64));
+        a.add(x, SOFTMAX ? __shfl_xor(a.M, by, 64) : 0.f, SOFTMAX ? __shfl_xor(a.l, by, 64) : 0.f);
+      }
+      const int r = r0 + 4 * i;
+      if (group == 0 && r < it.n_rows)
+        *reinterpret_cast<uint2*>(p.out + (int64_t)(it.u.row0 + it.first_row + r) * p.out_stride + f) =
+            sum[i].template out<H>(attend_seen(it.u, it.first_row + r, p.causal));
     }
   }
 }
@@ -375,10 +447,12 @@ __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend8_kernel(AttendPar
     __syncthreads();
   }
   if (wave == 0) attend8_store<H, DH, NQ, SOFTMAX>(p, it, 0, lane, seen, oacc, mref, lsum);
+  if constexpr (USERS <= kFewAttendUsers) {
+    if (p.arrived != nullptr && u.parts() > 1) attend8_join_last<H, DH, SOFTMAX>(p, it, wave, lane);
+  }
 }
 
-// Adds the pieces of rows that were cut along the keys, in their order, and writes the rows.  One wavefront for 256 features of a row (four to a lane); the
-// pieces are loaded eight at a time.
+// The same as a launch of its own: one wavefront for 256 features of a row, pieces loaded eight at a time.
 struct JoinUser {
   int32_t row0, rows, keys, part0, parts;
   int32_t cut0;        // rows of the launch's users before it
@@ -390,8 +464,9 @@ template <int USERS> struct JoinParams {
   int32_t n_users, n_rows, d, n_heads, causal;
   JoinUser users[USERS];
 };
-template <typename H, bool SOFTMAX, int USERS>
+template <typename H, int DH, bool SOFTMAX, int USERS>
 __global__ __launch_bounds__(256) void attend8_join_kernel(JoinParams<USERS> p) {
+  constexpr int GROUPS = 256 / DH;
   const int lane = threadIdx.x & 63, segs_sh = max(__builtin_ctz(p.d) - 8, 0);
   const int unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
   const int row = unit >> segs_sh, f = (unit - (row << segs_sh)) * 256 + lane * 4;
@@ -405,11 +480,10 @@ __global__ __launch_bounds__(256) void attend8_join_kernel(JoinParams<USERS> p) 
   const JoinUser u = p.users[__builtin_amdgcn_readfirstlane(at)];
   const int r = row - u.cut0, seen = p.causal ? max(u.keys - u.rows + 1 + r, 0) : u.keys;
   const bool mine = f < p.d;           // (d = 128: half of the lanes)
-  const int head = (mine ? f : 0) / (p.d / p.n_heads);
+  const int head = (mine ? f : 0) / DH;
   const float* x = p.part + ((int64_t)u.part0 + r) * p.d + (mine ? f : 0);
   const int64_t step = (int64_t)u.rows * p.d;      // between a row's pieces
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  float M = -INFINITY, l = 0.f;
+  PieceSum<SOFTMAX> sum[GROUPS];
   for (int k0 = 0; k0 < u.parts; k0 += 8) {
     float4 v[8];
     float2 ml[8];
@@ -417,26 +491,17 @@ __global__ __launch_bounds__(256) void attend8_join_kernel(JoinParams<USERS> p) 
     for (int k = 0; k < 8; ++k) {
       const int kk = min(k0 + k, u.parts - 1);
       v[k] = *reinterpret_cast<const float4*>(x + kk * step);
-      if constexpr (SOFTMAX) ml[k] = *reinterpret_cast<const float2*>(p.ml + (((int64_t)u.part0 + (int64_t)kk * u.rows + r) * p.n_heads + head) * 2);
+      ml[k] = SOFTMAX ? *reinterpret_cast<const float2*>(p.ml + (((int64_t)u.part0 + (int64_t)kk * u.rows + r) * p.n_heads + head) * 2) : make_float2(0.f, 0.f);
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      if (k0 + k >= u.parts) continue;
-      if constexpr (SOFTMAX) {
-        const float mn = fmaxf(M, ml[k].x), c0 = M == mn ? 1.0f : __builtin_amdgcn_exp2f(M - mn), c1 = ml[k].x == mn ? 1.0f : __builtin_amdgcn_exp2f(ml[k].x - mn);
-        o = make_float4(o.x * c0 + v[k].x * c1, o.y * c0 + v[k].y * c1, o.z * c0 + v[k].z * c1, o.w * c0 + v[k].w * c1);
-        l = l * c0 + ml[k].y * c1;
-        M = mn;
-      } else {
-        o = make_float4(o.x + v[k].x, o.y + v[k].y, o.z + v[k].z, o.w + v[k].w);
-      }
-    }
+    for (int k = 0; k < 8; ++k)
+      if (k0 + k < u.parts) sum[k % GROUPS].add(v[k], ml[k].x, ml[k].y);
   }
-  if (!mine) return;
-  const float mul = SOFTMAX ? 1.0f / l : 0.69314718055994531f / (float)seen;
-  uint2 w = make_uint2(H::pack2(o.x * mul, o.y * mul), H::pack2(o.z * mul, o.w * mul));
-  if (seen == 0) w = make_uint2(0, 0);
-  *reinterpret_cast<uint2*>(p.out + (int64_t)(u.row0 + r) * p.out_stride + f) = w;
+#pragma unroll
+  for (int by = 1; by < GROUPS; by *= 2)
+#pragma unroll
+    for (int i = 0; i < GROUPS; i += 2 * by) sum[i].add(sum[i + by].o, sum[i + by].M, sum[i + by].l);
+  if (mine) *reinterpret_cast<uint2*>(p.out + (int64_t)(u.row0 + r) * p.out_stride + f) = sum[0].template out<H>(seen);
 }
 
 }  // namespace relaygr

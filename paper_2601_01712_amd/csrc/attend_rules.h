@@ -26,6 +26,10 @@ inline int attend_parts(int nk, int piece) {
   return (nk + per - 1) / per;
 }
 
+// Whether a launch of few users joins the pieces of its rows itself, the last workgroup of an item's to arrive, or leaves that to a second launch, which takes 3.3 us of
+// the host and 2 of the GPU but has all of the chip for it.  most_sums: rows of an item times its pieces, at most.
+inline bool attend_joins_itself(int most_sums, int64_t items, int counters) { return most_sums <= 256 && items <= counters; }
+
 // A workgroup is four wavefronts that share an item's key tiles, and two or three of them a compute unit are full speed.
 //
 // Two blocks of 32 rows an item (one conversion of the codes for twice the rows) where the launch still has four items a compute unit and users have

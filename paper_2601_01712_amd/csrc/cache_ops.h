@@ -20,7 +20,11 @@ struct AttendCall {
   int n_cus;
   char* scratch;
   size_t scratch_bytes;
+  uint32_t* arrived;      // kArrivals counters, zero; null: the call may not use them (its stream is under capture)
 };
+// Counters of pieces that have arrived (attend8.h), behind a context's packed weights.  A call leaves them as it found them, zero, and a context's calls
+// follow one another on the GPU; replays of captured graphs are not the library's to order, so that captured calls join by a launch of their own.
+constexpr int kArrivals = 4096;
 // A user's K and V of one layer, as 16-bit tiles in scratch, on their way into its 8-bit entry.
 struct TilesJob { int64_t page0; int32_t tiles; const void* src; };
 int quantise_tiles(const KvPool* pool, int layer, const TilesJob* jobs, int n_jobs, hipStream_t st);

@@ -183,13 +183,16 @@ int relaygr::attend8(KvPool* pool, const AttendCall& c, hipStream_t st) {
   const bool once = rule.once;
   const size_t row_bytes = (size_t)d * 4 + (c.softmax ? (size_t)H * 8 : 0);
   int64_t partial_rows;
+  int most_sums;      // rows of an item times its pieces
   for (;; rule.piece = rule.piece > 1 << 20 ? 0 : 2 * rule.piece) {      // (0: nothing is cut)
     partial_rows = 0;
+    most_sums = 0;
     for (Work& w : work) {
       const int nk = (w.keys + kTile - 1) / kTile;
       w.parts = attend_parts(nk, rule.piece);
       w.per = std::max(1, (nk + w.parts - 1) / w.parts);
       if (w.parts > 1) partial_rows += (int64_t)w.parts * w.rows;
+      most_sums = std::max(most_sums, std::min(w.rows, item_rows) * w.parts);
     }
     if (partial_rows == 0 || ((size_t)partial_rows * row_bytes <= c.scratch_bytes && partial_rows < (1ll << 31))) break;
   }
@@ -222,15 +225,16 @@ int relaygr::attend8(KvPool* pool, const AttendCall& c, hipStream_t st) {
         j.n_rows += w.rows;
         part0 += w.parts * w.rows;
       }
+      if (USERS == kFewAttendUsers && c.arrived && attend_joins_itself(most_sums, (int64_t)p.n_items * H, kArrivals)) p.arrived = c.arrived;
       by_head(cfg, [&](auto h, auto dim) {
         using HT = decltype(h);
         constexpr int DH = decltype(dim)::value;
         if (c.softmax) launch_attend<HT, DH, true>(p, blocks, once, st);
         else launch_attend<HT, DH, false>(p, blocks, once, st);
-        if (j.n_users == 0) return;
+        if (j.n_users == 0 || p.arrived) return;
         const dim3 grid((unsigned)(((int64_t)j.n_rows * std::max(1, d / 256) + 3) / 4));
-        if (c.softmax) hipLaunchKernelGGL((attend8_join_kernel<HT, true, USERS>), grid, dim3(256), 0, st, j);
-        else hipLaunchKernelGGL((attend8_join_kernel<HT, false, USERS>), grid, dim3(256), 0, st, j);
+        if (c.softmax) hipLaunchKernelGGL((attend8_join_kernel<HT, DH, true, USERS>), grid, dim3(256), 0, st, j);
+        else hipLaunchKernelGGL((attend8_join_kernel<HT, DH, false, USERS>), grid, dim3(256), 0, st, j);
       });
       LAUNCH_CHECK(what);
     }

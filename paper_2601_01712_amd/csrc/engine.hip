@@ -117,11 +117,13 @@ struct Plan {
 static int rows_per_attn_tile(const relaygr_model_config& c, int nq) { return c.dtype == RELAYGR_DTYPE_FP32 ? 32 : 128 * nq; }
 
 // Lays the call's buffers out in scratch.  Everything is a function of the counts already in p.
-// Bytes at the start of scratch that hold the weights re-packed into MFMA panels (bf16 only).
+// Bytes at the start of scratch that a context keeps (16-bit types only): the weights re-packed into MFMA panels, and behind them the counters of
+// attention over 8-bit caches.
+constexpr size_t kArrivalBytes = kArrivals * sizeof(uint32_t);
 static size_t wpack_bytes(const relaygr_model_config& c) {
   if (!is_half16(c)) return 0;
   const size_t d = c.d_model;
-  return align_up((size_t)c.n_layers * 5 * d * d * 2);
+  return align_up((size_t)c.n_layers * 5 * d * d * 2) + kArrivalBytes;
 }
 
 // Prefix rows of a user start at a multiple of this in the row space (bf16: GEMM tiles of 256 rows
@@ -340,7 +342,8 @@ extern "C" int relaygr_ctx_create(const relaygr_model_config* cfg, const relaygr
       c->w1_packed.push_back(w1p);
       c->w2_packed.push_back(w2p);
     }
-    hipError_t e = hipDeviceSynchronize();
+    hipError_t e = hipMemset((char*)scratch_dev + wpack_bytes(*cfg) - kArrivalBytes, 0, kArrivalBytes);
+    if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e != hipSuccess) { delete c; return fail(RELAYGR_EHIP, "ctx_create: packing weights: %s", hipGetErrorString(e)); }
   }
   // Pinned staging for the per-call descriptor blob, sized once from what the scratch buffer can hold: a call
@@ -1121,8 +1124,9 @@ extern "C" int relaygr_cache_attend(relaygr_ctx* c, relaygr_kv_pool* pool, int32
   std::lock_guard<std::mutex> call_lock(c->mu);
   hipStream_t st = (hipStream_t)hip_stream;
   const size_t wp = wpack_bytes(c->cfg);
-  const AttendCall call = {rows, layer, causal, q, q_stride, out, out_stride, c->attn_form == RELAYGR_ATTN_SOFTMAX, c->n_cus, c->scratch + wp, c->scratch_bytes - wp};
   const bool capturing = stream_is_capturing(st);      // (as in run)
+  const AttendCall call = {rows, layer, causal, q, q_stride, out, out_stride, c->attn_form == RELAYGR_ATTN_SOFTMAX, c->n_cus, c->scratch + wp, c->scratch_bytes - wp,
+                           capturing ? nullptr : (uint32_t*)(c->scratch + wp - kArrivalBytes)};
   if (!capturing && c->has_call && c->last_stream != st) HIP_TRY(order_behind(st, c->last_stream, c->call_done));
   int rc;
   try { rc = attend8(kp, call, st); } catch (...) { rc = fail(RELAYGR_EINVAL, "cache_attend: out of host memory"); }
