@@ -41,12 +41,6 @@ template <int USERS> struct AttendParams {
 // Tokens that row i of the user sees.
 __device__ __forceinline__ int attend_seen(const AttendUser& u, int i, int causal) { return causal ? max(u.keys - u.rows + 1 + i, 0) : u.keys; }
 
-template <bool ONCE>
-__device__ __forceinline__ uint4 load16(const char* p) {
-  const u32x4_t* x = reinterpret_cast<const u32x4_t*>(p);
-  return __builtin_bit_cast(uint4, ONCE ? __builtin_nontemporal_load(x) : *x);
-}
-
 // NaN codes of four, as 0x01 in their bytes.
 __device__ __forceinline__ uint32_t fp8_nans(uint32_t codes) { return (((codes & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u; }
 
@@ -101,13 +95,7 @@ __device__ __forceinline__ bool attend8_item(const AttendParams<USERS>& p, int l
     item = (turn << (3 - heads_sh)) + (xcd >> heads_sh);
   }
   if (item >= p.n_items) return false;
-  int at = -1;                     // the last user whose items begin at or before this one
-#pragma unroll
-  for (int u0 = 0; u0 < USERS; u0 += 64) {
-    const bool there = u0 + lane < p.n_users;
-    at += __builtin_popcountll(__builtin_amdgcn_ballot_w64(there && p.users[there ? u0 + lane : 0].item0 <= item));
-  }
-  it->u = p.users[__builtin_amdgcn_readfirstlane(at)];
+  it->u = p.users[last_at_or_before<USERS>(p.n_users, item, lane, [&](int i) { return p.users[i].item0; })];
   const int row_tiles = (it->u.rows + ROWS - 1) / ROWS;
   it->piece = (item - it->u.item0) / row_tiles;
   it->first_row = (item - it->u.item0 - it->piece * row_tiles) * ROWS;
@@ -471,13 +459,7 @@ __global__ __launch_bounds__(256) void attend8_join_kernel(JoinParams<USERS> p) 
   const int unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
   const int row = unit >> segs_sh, f = (unit - (row << segs_sh)) * 256 + lane * 4;
   if (row >= p.n_rows) return;
-  int at = -1;
-#pragma unroll
-  for (int u0 = 0; u0 < USERS; u0 += 64) {
-    const bool there = u0 + lane < p.n_users;
-    at += __builtin_popcountll(__builtin_amdgcn_ballot_w64(there && p.users[there ? u0 + lane : 0].cut0 <= row));
-  }
-  const JoinUser u = p.users[__builtin_amdgcn_readfirstlane(at)];
+  const JoinUser u = p.users[last_at_or_before<USERS>(p.n_users, row, lane, [&](int i) { return p.users[i].cut0; })];
   const int r = row - u.cut0, seen = p.causal ? max(u.keys - u.rows + 1 + r, 0) : u.keys;
   const bool mine = f < p.d;           // (d = 128: half of the lanes)
   const int head = (mine ? f : 0) / DH;

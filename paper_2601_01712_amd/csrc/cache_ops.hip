@@ -41,8 +41,8 @@ int resolve_rows(const char* what, KvPool* pool, int32_t layer, const relaygr_kv
   for (int u = 0; u < r->n_users; ++u)
     if (r->row_off[u + 1] < r->row_off[u]) return fail(RELAYGR_EINVAL, "%s: row offsets not monotone at user %d", what, u);
   entries->resize(r->n_users);
-  for (int u = 0; u < r->n_users; ++u)
-    if (pool->resolve(r->handles[u], &(*entries)[u]) != RELAYGR_OK) return fail(RELAYGR_ENOENT, "%s: user %d: stale or unknown handle", what, u);
+  const int found = pool->resolve_all(r->handles, r->n_users, entries->data());
+  if (found < r->n_users) return fail(RELAYGR_ENOENT, "%s: user %d: stale or unknown handle", what, found);
   return RELAYGR_OK;
 }
 
@@ -60,37 +60,40 @@ void by_head(const relaygr_model_config& cfg, F launch) {
   else by_dh(Bf16());
 }
 
-char* entry_tile0(const KvPool* pool, const PoolEntry& e) {
-  return (char*)pool->slab + (size_t)e.page0 * pool->page_bytes;
-}
-
+// once: rows and codes are more than the caches hold.
 template <bool WRITE, int USERS>
 int launch_rows(const char* what, const KvPool* pool, int layer, const relaygr_kv_rows* r, const std::vector<PoolEntry>& entries, void* k, int64_t k_stride,
-                void* v, int64_t v_stride, hipStream_t st) {
+                void* v, int64_t v_stride, bool once, hipStream_t st) {
   const relaygr_model_config& cfg = pool->cfg;
   RowsParams<USERS> p = {};
   p.k = k; p.v = v; p.k_stride = k_stride; p.v_stride = v_stride;
-  p.tile_stride = pool->tile_stride;
+  p.slab = (char*)pool->slab; p.page_bytes = (int64_t)pool->page_bytes; p.tile_stride = pool->tile_stride;
   p.codes_off = layer * pool->layer_stride;
   p.scales_off = q8_scales_off(cfg, layer);
-  p.n_heads = cfg.n_heads;
+  p.d = cfg.d_model;
   for (int u = 0; u < r->n_users;) {
     p.n_users = 0; p.n_tiles = 0;
     for (; u < r->n_users && p.n_users < USERS; ++u) {
       const int32_t first = r->first_token ? r->first_token[u] : 0, n = r->row_off[u + 1] - r->row_off[u];
       if (n == 0) continue;
-      p.users[p.n_users++] = {entry_tile0(pool, entries[u]), first, n, r->row_off[u], p.n_tiles, 0};
+      p.users[p.n_users++] = {(int32_t)entries[u].page0, first, n, r->row_off[u], p.n_tiles};
       p.n_tiles += (int)(((int64_t)first + n - 1) / kTile - first / kTile + 1);
     }
     if (p.n_users == 0) break;
-    const dim3 grid((unsigned)(((int64_t)p.n_tiles * cfg.n_heads * 2 + 3) / 4));
-    auto launch = [&](auto h, auto dim) {
+    by_head(cfg, [&](auto h, auto dim) {
       using H = decltype(h);
-      constexpr int DH = decltype(dim)::value;
-      if (WRITE) hipLaunchKernelGGL((kv8_write_kernel<H, DH, USERS>), grid, dim3(256), 0, st, p);
-      else hipLaunchKernelGGL((kv8_read_kernel<H, DH, USERS>), grid, dim3(256), 0, st, p);
-    };
-    by_head(cfg, launch);
+      constexpr int DH = decltype(dim)::value, FW = DH < 64 ? 64 : DH;      // (runs of 128 bytes of a row at least)
+      const dim3 grid((unsigned)(((int64_t)p.n_tiles * (cfg.d_model / FW) * 2 + 3) / 4));
+      auto go = [&](auto once) {
+        constexpr bool ONCE = decltype(once)::value;
+        if (WRITE) hipLaunchKernelGGL((kv8_write_kernel<H, DH, FW, ONCE, USERS>), grid, dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((kv8_read_kernel<H, DH, FW, ONCE, USERS>), grid, dim3(256), 0, st, p);
+      };
+      if constexpr (USERS > kFewRowUsers) {
+        if (once) { go(std::true_type()); return; }
+      }
+      go(std::false_type());
+    });
     LAUNCH_CHECK(what);
   }
   return RELAYGR_OK;
@@ -110,15 +113,19 @@ int move_rows(const char* what, KvPool* pool, int32_t layer, const relaygr_kv_ro
   const relaygr_model_config& cfg = pool->cfg;
   if ((rc = check_rows_array(what, "k", k, k_stride, cfg.d_model)) != RELAYGR_OK) return rc;
   if ((rc = check_rows_array(what, "v", v, v_stride, cfg.d_model)) != RELAYGR_OK) return rc;
-  if (WRITE) {   // two users writing one entry would race
+  if (WRITE && r->n_users > 1) {   // two users writing one entry would race
     std::vector<relaygr_kv_handle> hs;
+    hs.reserve(r->n_users);
     for (int u = 0; u < r->n_users; ++u) if (r->row_off[u + 1] > r->row_off[u]) hs.push_back(r->handles[u]);
     std::sort(hs.begin(), hs.end());
     if (std::adjacent_find(hs.begin(), hs.end()) != hs.end()) return fail(RELAYGR_EINVAL, "%s: two users of the batch carry the same handle", what);
   }
   (void)hipGetLastError();   // a failure the caller's own HIP calls left behind is not this call's
-  if (r->n_users <= kFewRowUsers) return launch_rows<WRITE, kFewRowUsers>(what, pool, layer, r, entries, k, k_stride, v, v_stride, st);
-  return launch_rows<WRITE, kRowUsers>(what, pool, layer, r, entries, k, k_stride, v, v_stride, st);
+  // (us without / with the hint to leave nothing in the caches, write and read, d = 256, 64 users of 4096 tokens, 402 MB: 78.2 / 65.9, 76.8 / 72.6; d = 512, 64 of 3600,
+  // 708 MB: 141 / 145, 142 / 133; d = 1024, 16 of 4096: 78.9 / 69.9, 82.3 / 74.3; 16 of 1000, 49 MB: 10.7 / 11.4, 10.4 / 9.9)
+  const bool once = (int64_t)r->row_off[r->n_users] * cfg.d_model * 6 >= kOnceBytes;
+  if (r->n_users <= kFewRowUsers && !once) return launch_rows<WRITE, kFewRowUsers>(what, pool, layer, r, entries, k, k_stride, v, v_stride, once, st);
+  return launch_rows<WRITE, kRowUsers>(what, pool, layer, r, entries, k, k_stride, v, v_stride, once, st);
 }
 
 template <typename H, int DH, bool SM, int USERS>
@@ -144,7 +151,7 @@ int relaygr::quantise_tiles(const KvPool* pool, int layer, const TilesJob* jobs,
   p.codes_off = layer * pool->layer_stride; p.scales_off = q8_scales_off(cfg, layer); p.n_heads = cfg.n_heads;
   for (int j = 0; j < n_jobs;) {
     p.n_users = 0; p.n_tiles = 0;
-    for (; j < n_jobs && p.n_users < kRowUsers; ++j) {
+    for (; j < n_jobs && p.n_users < kTilesUsers; ++j) {
       p.users[p.n_users++] = {(char*)pool->slab + (size_t)jobs[j].page0 * pool->page_bytes, (const uint16_t*)jobs[j].src, p.n_tiles, 0};
       p.n_tiles += jobs[j].tiles;
     }

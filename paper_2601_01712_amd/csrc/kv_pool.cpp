@@ -82,6 +82,16 @@ int KvPool::resolve(relaygr_kv_handle h, PoolEntry* out) {
   return RELAYGR_OK;
 }
 
+int KvPool::resolve_all(const relaygr_kv_handle* h, int n, PoolEntry* out) {
+  std::lock_guard<std::mutex> lk(mu);
+  for (int i = 0; i < n; ++i) {
+    uint32_t slot, gen;
+    if (!split_handle(h[i], &slot, &gen) || slot >= entries.size() || !entries[slot].live || entries[slot].generation != gen) return i;
+    out[i] = entries[slot];
+  }
+  return n;
+}
+
 void KvPool::stats(int64_t* total, int64_t* free_pages, int64_t* live, int64_t* largest) {
   std::lock_guard<std::mutex> lk(mu);
   int64_t f = 0, big = 0;

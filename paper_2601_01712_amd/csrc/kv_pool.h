@@ -42,12 +42,14 @@ struct KvPool {
   std::vector<uint32_t> free_slots;
   std::unordered_map<uint64_t, uint32_t> by_user;
 
-  // All four return RELAYGR_* codes and are thread-safe.
+  // All four return RELAYGR_* codes; these calls are thread-safe.
   int alloc(uint64_t user_id, int32_t prefix_len, relaygr_kv_handle* out);
   int release(relaygr_kv_handle h);
   int lookup(uint64_t user_id, relaygr_kv_handle* out);
   // Copies the live entry of h into *e (RELAYGR_ENOENT if stale).
   int resolve(relaygr_kv_handle h, PoolEntry* e);
+  // The same for n handles at once; how many of them, from the first on, are live (n: all, and all are copied).
+  int resolve_all(const relaygr_kv_handle* h, int n, PoolEntry* e);
   void stats(int64_t* total, int64_t* free_pages, int64_t* live, int64_t* largest);
 };
 
