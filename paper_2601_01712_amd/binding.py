@@ -403,27 +403,16 @@ def _kv_rows_array(what: str, pool: KvPool, rows: KvRows, t: torch.Tensor):
     return (t.data_ptr() if n else None), (stride[0] if n > 1 else d)
 
 
-class _KvCall:
-    """Where a call's work and results go: a stream (default: the current one of the pool's device), with that device current.  Entered only
-    where the caller's state is not that already: torch's guards take several microseconds."""
-
-    def __init__(self, pool: KvPool, stream):
-        device = pool.slab.device
-        if stream is None:
-            self.raw = torch._C._cuda_getCurrentRawStream(device.index)
-            self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-        else:
-            s = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
-            self.raw, self.guard = s.cuda_stream, torch.cuda.stream(s)      # (results are allocated on the stream that writes them)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.raw
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _kv_guard(pool: KvPool, stream):
+    """What a call has to be made under to be the default one, of the current stream of the pool's device, which is also where its results are
+    allocated; None if it is that already (torch's guards take several microseconds)."""
+    device = pool.slab.device
+    if stream is not None:
+        s = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
+        if s.device != device:
+            raise RelayGRError(RELAYGR_EINVAL, f"a stream of {s.device} for a pool on {device}")
+        return torch.cuda.stream(s)
+    return None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
 
 def _result_rows(what: str, pool: KvPool, rows: KvRows, t: Optional[torch.Tensor]):
@@ -437,29 +426,39 @@ def _result_rows(what: str, pool: KvPool, rows: KvRows, t: Optional[torch.Tensor
 
 def relaygr_kv_pool_write(pool: KvPool, layer: int, rows: KvRows, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
     """Quantises rows of K and V ([rows, d_model] or [rows, heads, d_head]) into the entries' tokens first_token on."""
+    guard = _kv_guard(pool, stream)
+    if guard is not None:
+        with guard:
+            return relaygr_kv_pool_write(pool, layer, rows, k, v)
     kp, ks = _kv_rows_array("kv_pool_write: k", pool, rows, k)
     vp, vs = _kv_rows_array("kv_pool_write: v", pool, rows, v)
-    with _KvCall(pool, stream) as st:
-        _check(load_library().relaygr_kv_pool_write(pool.handle, layer, rows.ref, kp, ks, vp, vs, st))
+    _check(load_library().relaygr_kv_pool_write(pool.handle, layer, rows.ref, kp, ks, vp, vs, torch._C._cuda_getCurrentRawStream(pool.slab.device.index)))
 
 
 def relaygr_kv_pool_read(pool: KvPool, layer: int, rows: KvRows, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
                          stream=None):
     """(k, v): the values that tokens of the entries stand for, [rows, d_model] each (made here if not given)."""
-    with _KvCall(pool, stream) as st:
-        k, kp, ks = _result_rows("kv_pool_read: k", pool, rows, k)
-        v, vp, vs = _result_rows("kv_pool_read: v", pool, rows, v)
-        _check(load_library().relaygr_kv_pool_read(pool.handle, layer, rows.ref, kp, ks, vp, vs, st))
+    guard = _kv_guard(pool, stream)
+    if guard is not None:
+        with guard:
+            return relaygr_kv_pool_read(pool, layer, rows, k, v)
+    k, kp, ks = _result_rows("kv_pool_read: k", pool, rows, k)
+    v, vp, vs = _result_rows("kv_pool_read: v", pool, rows, v)
+    _check(load_library().relaygr_kv_pool_read(pool.handle, layer, rows.ref, kp, ks, vp, vs, torch._C._cuda_getCurrentRawStream(pool.slab.device.index)))
     return k, v
 
 
 def relaygr_cache_attend(ctx: Context, pool: KvPool, layer: int, rows: KvRows, q: torch.Tensor, causal: bool = False,
                          out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """One layer's attention of query rows over entries of an 8-bit pool, in the context's form: [rows, d_model] (made here if not given)."""
+    guard = _kv_guard(pool, stream)
+    if guard is not None:
+        with guard:
+            return relaygr_cache_attend(ctx, pool, layer, rows, q, causal, out)
     qp, qs = _kv_rows_array("cache_attend: q", pool, rows, q)
-    with _KvCall(pool, stream) as st:
-        out, op, os_ = _result_rows("cache_attend: out", pool, rows, out)
-        _check(load_library().relaygr_cache_attend(ctx.handle, pool.handle, layer, rows.ref, int(causal), qp, qs, op, os_, st))
+    out, op, os_ = _result_rows("cache_attend: out", pool, rows, out)
+    _check(load_library().relaygr_cache_attend(ctx.handle, pool.handle, layer, rows.ref, int(causal), qp, qs, op, os_,
+                                               torch._C._cuda_getCurrentRawStream(pool.slab.device.index)))
     return out
 
 
