@@ -223,7 +223,9 @@ __device__ __forceinline__ void softmax_track(const f32x16_t (&s)[NQ], const int
 // Q8: prefix tiles come from an 8-bit pool (kv8.h) where a user has an entry there; recomputed prefixes and suffixes are 16-bit tiles as ever.
 // A tile of codes passes through registers: each thread has its share of the next tile but one on its way while the workgroup works on a
 // tile, and turns it into the 16-bit tile's LDS image, which holds exactly what the codes stand for, when the ring slot becomes free.  Half the bytes of K/V
-// for 1/NW of a tile's conversions per wavefront (dh = 64, four wavefronts: 16 instructions and four LDS stores beside about 1800 cycles of SiLU).
+// for 1/NW of a tile's conversions per wavefront (dh = 64, four wavefronts: 16 instructions and four LDS stores), which are in the way of wavefronts that
+// have their SIMD to themselves and of no weight where two share it.  us a ranking on a 16-bit / on an 8-bit pool, d = 512, 8 layers: 128 users of 8192 keys and 32
+// candidates 3259 / 2882, of one 2993 / 2775; 16 of 4096 and 512 993 / 1003; one of 4096 and 512 232 / 249, of 2000 and 100 191 / 195.
 template <typename H, int DH, int NQ, int NW, bool SOFTMAX, int GS = 1, bool Q8 = false>
 __global__ __launch_bounds__(NW * GS * 64, (DH >= 128 || GS > 1) ? 1 : 512 / (NW * 64)) void attn_bf16_kernel(AttnParams p) {   // DH = 128: the 96 KiB tile ring admits one workgroup per compute unit
   constexpr int KS = DH / 16;              // k-steps of the first product
@@ -386,23 +388,26 @@ __global__ __launch_bounds__(NW * GS * 64, (DH >= 128 || GS > 1) ? 1 : 512 / (NW
   const char* kv8_base = reinterpret_cast<const char*>(at.kv) + (int64_t)p.layer * at.layer_stride(p.d) + (int64_t)head * TILE;
   const int gtid = wave * 64 + lane;
   uint4 raw[CH8];
-  float2 raw_scale = make_float2(1.f, 1.f);
-  auto fetch8 = [&](int tt, uint4 (&x)[CH8], float2& scale) {
+  float raw_scale[CH8];     // (a load for each lane: as scalar loads they would count with the LDS reads, whose every wait would be for them too)
+  const bool k_chunk = wave < NW / 2;        // CH8 = 1: the first wavefronts have K's chunks; else the first half of each thread's are K's
+  auto fetch8 = [&](int tt, uint4 (&x)[CH8], float (&scale)[CH8]) {
     if (!has8 || tt >= tr.nkp) return;
     const char* tile = kv8_base + (int64_t)tt * at.kv_tile_stride;
-    scale = *reinterpret_cast<const float2*>(tile + p.scales_off - (int64_t)head * TILE + head * 8);
+    // (through descriptors: the base is a pointer that was itself loaded, whose plain loads would be flat ones)
+    const BufferView codes(tile, TILE), scales(tile + p.scales_off - (int64_t)head * TILE + head * 8, 8);
 #pragma unroll
-    for (int i = 0; i < CH8; ++i) x[i] = *reinterpret_cast<const uint4*>(tile + (i * (NW * 64) + gtid) * 16);
+    for (int c = 0; c < CH8; ++c) {
+      x[c] = codes.load(gtid * 16, c * (NW * 64 * 16));
+      scale[c] = scales.load_f32((CH8 == 1 ? k_chunk : c < CH8 / 2) ? 0 : 4);
+    }
   };
-  auto place8 = [&](int tt, int b, const uint4 (&x)[CH8], const float2& scale) {
+  auto place8 = [&](int tt, int b, const uint4 (&x)[CH8], const float (&scale)[CH8]) {
     if (!has8 || tt >= tr.nkp) { issue_tile(tt, b); return; }
 #pragma unroll
     for (int i = 0; i < CH8; ++i) {
-      const int c = i * (NW * 64) + gtid;
-      const float sc = c < 4 * DH ? scale.x : scale.y;
-      uint16_t* dst = &bufs[b][(c >> 6) * 1024 + lane * 8];
-      *reinterpret_cast<u32x4_t*>(dst) = fp8_frag<H>(x[i].x, x[i].y, sc);
-      *reinterpret_cast<u32x4_t*>(dst + 512) = fp8_frag<H>(x[i].z, x[i].w, sc);
+      uint16_t* dst = &bufs[b][((i * (NW * 64) + gtid) >> 6) * 1024 + lane * 8];
+      *reinterpret_cast<u32x4_t*>(dst) = fp8_frag<H>(x[i].x, x[i].y, scale[i]);
+      *reinterpret_cast<u32x4_t*>(dst + 512) = fp8_frag<H>(x[i].z, x[i].w, scale[i]);
     }
   };
 
@@ -416,15 +421,17 @@ __global__ __launch_bounds__(NW * GS * 64, (DH >= 128 || GS > 1) ? 1 : 512 / (NW
   if (nt == 0) start_from_own_key();
   if (nt > 0) {
     if constexpr (Q8) {
-      uint4 raw1[CH8];
-      float2 scale1 = make_float2(1.f, 1.f);
-      fetch8(tr.t0, raw, raw_scale);
+      // (the third tile's codes are asked for with the first two's: they are waited for before the first product, whose operands the compiler
+      // takes for what 16-bit tiles on their way to LDS may write)
+      uint4 raw0[CH8], raw1[CH8];
+      float scale0[CH8], scale1[CH8];
+      fetch8(tr.t0, raw0, scale0);
       if (nt > 1) fetch8(tr.t0 + 1, raw1, scale1);
+      if (nt > 2) fetch8(tr.t0 + 2, raw, raw_scale);
       start_from_own_key();
-      place8(tr.t0, 0, raw, raw_scale);
+      place8(tr.t0, 0, raw0, scale0);
       if (nt > 1) place8(tr.t0 + 1, 1, raw1, scale1);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (16-bit tiles among them)
-      if (nt > 2) fetch8(tr.t0 + 2, raw, raw_scale);
     } else {
     issue_tile(tr.t0, 0);
     if (nt > 1) issue_tile(tr.t0 + 1, 1);
@@ -454,11 +461,12 @@ __global__ __launch_bounds__(NW * GS * 64, (DH >= 128 || GS > 1) ? 1 : 512 / (NW
     auto next_tile = [&](int i, int bn) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
+      const int free_slot = (bn == 2) ? 0 : bn + 1;
       if constexpr (Q8) {
-        if (i + 2 < nt) place8(tr.t0 + i + 2, (bn == 2) ? 0 : bn + 1, raw, raw_scale);
+        if (i + 2 < nt) place8(tr.t0 + i + 2, free_slot, raw, raw_scale);
         if (i + 3 < nt) fetch8(tr.t0 + i + 3, raw, raw_scale);
       } else if (i + 2 < nt) {
-        issue_tile(tr.t0 + i + 2, (bn == 2) ? 0 : bn + 1);
+        issue_tile(tr.t0 + i + 2, free_slot);
       }
     };
 
