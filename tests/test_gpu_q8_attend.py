@@ -252,3 +252,66 @@ def test_refusals():
     # no users, or no rows: nothing to do
     assert rg.relaygr_cache_attend(c.ctx, c.pool, 0, rg.KvRows([], [0]), c.q[:0]).shape == (0, 256)
     assert rg.relaygr_cache_attend(c.ctx, c.pool, 0, rg.KvRows(c.handles, [0, 0, 0]), c.q[:0]).shape == (0, 256)
+
+
+def test_entries_beyond_4_gib_of_the_slab():
+    """An entry behind more than 2^32 bytes of others, in the last of many layers."""
+    d, heads, dtype = 1024, 8, "bf16"
+    m = model(d, heads, dtype, "softmax", layers=16)
+    ctx = context_for(m, 1, 70)
+    tile = rg.relaygr_kv_pool_bytes_for_q8(ctx.cfg, 64, 64)
+    before = (1 << 32) // tile + 3
+    pool = rg.KvPool(ctx.cfg, dtype, (before + 4) * tile, 64, quantized=True)
+    rg.relaygr_kv_pool_alloc(pool, 1, before * 64)
+    h = rg.relaygr_kv_pool_alloc(pool, 2, 200)
+    assert rg.relaygr_kv_pool_locate(pool, h, 15, 199, 1023)[0] > 1 << 32
+    rng = np.random.default_rng(67)
+    (k, k64), (v, v64), (q, q64) = (values(rng, n, d, dtype) for n in (200, 200, 70))
+    rg.relaygr_kv_pool_write(pool, 15, rg.KvRows([h], [0, 200]), k.to(DEV), v.to(DEV))
+    kh, vh = held(k64.reshape(200, heads, -1), dtype), held(v64.reshape(200, heads, -1), dtype)
+    for got, want in zip(rg.relaygr_kv_pool_read(pool, 15, rg.KvRows([h], [0, 200])), (kh, vh)):
+        assert np.array_equal(got.double().cpu().numpy(), want.reshape(200, d))
+    out = rg.relaygr_cache_attend(ctx, pool, 15, rg.KvRows([h], [0, 70]), q.to(DEV))
+    want, bound = attend(q64.reshape(70, heads, -1), kh, vh, [200] * 70, "softmax", dtype)
+    assert (np.abs(out.double().cpu().numpy().reshape(want.shape) - want) <= bound).all()
+
+
+def test_calls_of_every_kind_in_turn_on_one_context():
+    """Cut calls that join themselves, captured ones that have a launch for it, and rankings, which use the same scratch: each leaves the others' results as they are."""
+    c = Case(256, 4, "bf16", "silu", [9000, 500, 64], [3, 20, 2], seed=71)
+    one = rg.KvRows(c.handles[:1], [0, 3])
+    many = rg.KvRows(c.handles, offsets(c.rows))
+    want = rg.relaygr_cache_attend(c.ctx, c.pool, 1, one, c.q[:3]), c.run()
+    c.check(want[1])
+    outs = torch.empty_like(want[0]), torch.empty_like(want[1])
+    graphs = []
+    for rows, q, out in ((one, c.q[:3], outs[0]), (many, c.q, outs[1])):
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            rg.relaygr_cache_attend(c.ctx, c.pool, 1, rows, q, out=out)
+    batch = rg.Batch({"n_users": 1, "user_ids": [7], "prefix_emb": np.zeros((0, 256), np.float32), "prefix_off": [0, 500],
+                      "suffix_emb": np.zeros((0, 256), np.float32), "suffix_off": [0, 0],
+                      "cand_emb": np.ones((20, 256), np.float32), "cand_off": [0, 20]}, "bf16", handles=[c.handles[1]])
+    for turn in range(3):
+        for out in outs:
+            out.zero_()
+        graphs[turn % 2].replay()
+        assert torch.equal(c.run(), want[1])
+        graphs[1 - turn % 2].replay()
+        rg.relaygr_rank_with_cache(c.ctx, c.pool, batch)
+        assert torch.equal(rg.relaygr_cache_attend(c.ctx, c.pool, 1, one, c.q[:3]), want[0])
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+def test_one_history_for_many_users_and_a_batch_with_idle_ones():
+    """The same entry in several users' places, users without rows between them."""
+    c = Case(256, 4, "fp16", "softmax", [300], [40], seed=73)
+    h = c.handles[0]
+    rows = rg.KvRows([h] * 5, [0, 10, 10, 25, 25, 40], key_len=[300, 5, 300, 300, 300])
+    out = rg.relaygr_cache_attend(c.ctx, c.pool, 1, rows, c.q)
+    c.check(out)
+    k, v = rg.relaygr_kv_pool_read(c.pool, 1, rg.KvRows([h, h], [0, 300, 400], first_token=[0, 100]))
+    assert torch.equal(k[300:], k[100:200]) and torch.equal(v[300:], v[100:200])
