@@ -95,7 +95,7 @@ __device__ __forceinline__ bool attend8_item(const AttendParams<USERS>& p, int l
     item = (turn << (3 - heads_sh)) + (xcd >> heads_sh);
   }
   if (item >= p.n_items) return false;
-  it->u = p.users[last_at_or_before<USERS>(p.n_users, item, lane, [&](int i) { return p.users[i].item0; })];
+  it->u = user_of(p.users, p.n_users, item, lane, [](const AttendUser& x) { return x.item0; });
   const int row_tiles = (it->u.rows + ROWS - 1) / ROWS;
   it->piece = (item - it->u.item0) / row_tiles;
   it->first_row = (item - it->u.item0 - it->piece * row_tiles) * ROWS;
@@ -459,7 +459,7 @@ __global__ __launch_bounds__(256) void attend8_join_kernel(JoinParams<USERS> p) 
   const int unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
   const int row = unit >> segs_sh, f = (unit - (row << segs_sh)) * 256 + lane * 4;
   if (row >= p.n_rows) return;
-  const JoinUser u = p.users[last_at_or_before<USERS>(p.n_users, row, lane, [&](int i) { return p.users[i].cut0; })];
+  const JoinUser u = user_of(p.users, p.n_users, row, lane, [](const JoinUser& x) { return x.cut0; });
   const int r = row - u.cut0, seen = p.causal ? max(u.keys - u.rows + 1 + r, 0) : u.keys;
   const bool mine = f < p.d;           // (d = 128: half of the lanes)
   const int head = (mine ? f : 0) / DH;

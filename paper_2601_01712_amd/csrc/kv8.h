@@ -176,16 +176,21 @@ struct RowsUser {
   int32_t row0;      // its first row in k and v
   int32_t unit0;     // touched tiles of the launch's users before it
 };
-// The last of USERS users, n of them there, whose `start` is at most x (the first one's is).
-template <int USERS, class Start>
-__device__ __forceinline__ int last_at_or_before(int n, int x, int lane, Start start) {
-  int at = -1;
+// Of n users with ascending starts the last whose `start` is at most x (the first one's is).  A launch of one has its first user from the arguments
+// at once, without the look at the starts in between.
+template <int USERS, class User, class Start>
+__device__ __forceinline__ User user_of(const User (&users)[USERS], int n, int x, int lane, Start start) {
+  User u = users[0];
+  if (n > 1) {
+    int at = -1;
 #pragma unroll
-  for (int u0 = 0; u0 < USERS; u0 += 64) {
-    const bool there = u0 + lane < n;
-    at += __builtin_popcountll(__builtin_amdgcn_ballot_w64(there && start(there ? u0 + lane : 0) <= x));
+    for (int u0 = 0; u0 < USERS; u0 += 64) {
+      const bool there = u0 + lane < n;
+      at += __builtin_popcountll(__builtin_amdgcn_ballot_w64(there && start(users[there ? u0 + lane : 0]) <= x));
+    }
+    u = users[__builtin_amdgcn_readfirstlane(at)];
   }
-  return __builtin_amdgcn_readfirstlane(at);
+  return u;
 }
 template <int USERS> struct RowsParams {
   void* k;           // [rows][stride] in the storage type: sources of a write, targets of a read
@@ -213,7 +218,7 @@ __device__ __forceinline__ bool rows_unit(const RowsParams<USERS>& p, int lane, 
   u->is_v = in_tile & 1;
   u->f0 = (in_tile >> 1) * FW;
   if (t >= p.n_tiles) return false;
-  const RowsUser us = p.users[last_at_or_before<USERS>(p.n_users, t, lane, [&](int i) { return p.users[i].unit0; })];
+  const RowsUser us = user_of(p.users, p.n_users, t, lane, [](const RowsUser& x) { return x.unit0; });
   const int tile = us.first / kTile + (t - us.unit0);
   u->r0 = max(us.first - tile * kTile, 0);
   u->r1 = min(us.first + us.rows - tile * kTile, kTile);
@@ -413,7 +418,7 @@ __global__ __launch_bounds__(256) void kv8_tiles_kernel(TilesParams p) {
   const int unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
   const int is_v = unit & 1, t = (unit >> 1) / p.n_heads, head = (unit >> 1) - t * p.n_heads;
   if (t >= p.n_tiles) return;
-  const TilesUser us = p.users[last_at_or_before<kTilesUsers>(p.n_users, t, lane, [&](int i) { return p.users[i].unit0; })];
+  const TilesUser us = user_of(p.users, p.n_users, t, lane, [](const TilesUser& x) { return x.unit0; });
   const uint4* src = reinterpret_cast<const uint4*>(us.src + (int64_t)(t - us.unit0) * p.src_stride + (2 * head + is_v) * (kTile * DH));
   char* tile = us.tile0 + (int64_t)(t - us.unit0) * p.tile_stride;
   uint4 x[NL];
