@@ -10,3 +10,4 @@ extern "C" void attend_rule_of(int n, const int32_t* rows, const int32_t* keys, 
   for (int u = 0; u < n; ++u) out[3] = std::max(out[3], (int32_t)relaygr::attend_parts((keys[u] + 63) / 64, r.piece));
 }
 extern "C" int attend_parts_of(int tiles, int piece) { return relaygr::attend_parts(tiles, piece); }
+extern "C" int attend_joins(int most_sums, int64_t items, int counters) { return relaygr::attend_joins_itself(most_sums, items, counters); }

@@ -315,3 +315,18 @@ def test_one_history_for_many_users_and_a_batch_with_idle_ones():
     c.check(out)
     k, v = rg.relaygr_kv_pool_read(c.pool, 1, rg.KvRows([h, h], [0, 300, 400], first_token=[0, 100]))
     assert torch.equal(k[300:], k[100:200]) and torch.equal(v[300:], v[100:200])
+
+
+@pytest.mark.parametrize("form", ["silu", "softmax"])
+def test_a_context_with_little_scratch(form):
+    """Rows are cut only as far as the scratch holds their partial sums: fewer pieces, or none, and the same answers."""
+    d, heads, lens, rows = 128, 1, [16384], [300]
+    parts = attend_rule(rows, lens, heads, d // heads)["parts"]
+    small = context_for(model(d, heads, "bf16", form), 1, 1)
+    weights = 2 * 5 * d * d * 2
+    assert parts > 1 and parts * rows[0] * d * 4 > rg.relaygr_scratch_bytes(small.cfg, 1, 0, 1) - weights
+    c = Case(d, heads, "bf16", form, lens, rows, seed=83)
+    c.check(c.run())
+    c.ctx = small
+    c.check(c.run())
+    c.check(c.run(causal=True), causal=True)

@@ -232,3 +232,42 @@ def test_calls_on_a_side_stream_and_results_made_there():
         side.synchronize()
         assert same(gk.double().cpu().numpy(), held(k64.reshape(1000, heads, d // heads), dtype))
         assert same(gv.double().cpu().numpy(), held(v64.reshape(1000, heads, d // heads), dtype))
+
+
+@pytest.mark.parametrize("dtype,d,heads", [("bf16", 256, 4), ("fp16", 256, 8), ("bf16", 1024, 8)])
+def test_batches_that_the_caches_do_not_hold(dtype, d, heads):
+    """128 MiB of rows and codes and more move by kernels that leave nothing in the caches: all of it written, its second part from the middle of a
+    block again, and read; three of the users against the definition."""
+    rng = np.random.default_rng(41)
+    users = 28
+    lens = [int(n) for n in rng.integers(3900, 4100, users) * 256 // d]
+    kept = [n - int(rng.integers(64, 200)) for n in lens]
+    cfg = rg.make_config(1, d, heads, dtype)
+    pool, handles = pool_for(cfg, dtype, lens)
+    at, pick = offsets(lens), (0, 11, users - 1)
+    assert sum(lens) * d * 6 >= 128 << 20
+    x = [torch.randn(sum(lens), d, device=DEV).to(TORCH[dtype]) for _ in range(2)]
+    rg.relaygr_kv_pool_write(pool, 0, rg.KvRows(handles, at), *x)
+    got = rg.relaygr_kv_pool_read(pool, 0, rg.KvRows(handles, at))
+    for g, t in zip(got, x):
+        for u in pick:
+            want = held(t[at[u]:at[u + 1]].double().cpu().numpy().reshape(lens[u], heads, d // heads), dtype)
+            assert same(g[at[u]:at[u + 1]].double().cpu().numpy(), want), u
+    # the users' last tokens eight times as large (launched with the others' unchanged ones, so that the batch is as large as before)
+    first = [k if u in pick else 0 for u, k in enumerate(kept)]
+    rows = offsets([n - f for n, f in zip(lens, first)])
+    part = [torch.cat([t[at[u] + first[u]:at[u + 1]] * (8.0 if u in pick else 1.0) for u in range(users)]) for t in x]
+    assert int(rows[-1]) * d * 6 >= 128 << 20
+    rg.relaygr_kv_pool_write(pool, 0, rg.KvRows(handles, rows, first_token=first), *part)
+    again = rg.relaygr_kv_pool_read(pool, 0, rg.KvRows(handles, at))
+    for g, before, t in zip(again, got, x):
+        for u in range(users):
+            a = slice(int(at[u]), int(at[u + 1]))
+            if u not in pick:
+                assert torch.equal(g[a], before[a]), u
+                continue
+            e = Entry(lens[u], heads, d // heads, dtype)
+            y = t[a].double().cpu().numpy().reshape(lens[u], heads, d // heads)
+            e.write(0, y)
+            e.write(first[u], 8.0 * y[first[u]:])
+            assert same(g[a].double().cpu().numpy(), e.x), u

@@ -194,3 +194,11 @@ def test_rule_of_the_attention_kernels():
     long_one = attend_rule([30] * 32, [1000] * 31 + [16384], 8, 64)
     assert long_one["parts"] > 4 and attend_rule([30] * 32, [1000] * 32, 8, 64)["parts"] == 1
     assert attend_rule([5], [0], 8, 64)["parts"] == 1
+
+
+def test_who_joins_the_pieces_of_few_users():
+    joins = rule_shim().attend_joins
+    joins.argtypes = [C.c_int, C.c_int64, C.c_int]
+    assert joins(64, 512, 4096) == 1 and joins(256, 4096, 4096) == 1
+    assert joins(257, 512, 4096) == 0                                    # many sums for one workgroup
+    assert joins(64, 4097, 4096) == 0                                    # more items than counters
