@@ -60,7 +60,8 @@
  *     d_model / 64.
  *   - In the 16-bit modes the first bytes of the scratch buffer hold the weights re-packed
  *     for the matrix cores (done once in relaygr_ctx_create, which synchronises the
- *     device); relaygr_scratch_bytes includes them.
+ *     device), and 16 KiB of counters for relaygr_cache_attend behind them; relaygr_scratch_bytes
+ *     includes them.
  */
 #ifndef RELAYGR_H
 #define RELAYGR_H
@@ -240,7 +241,8 @@ typedef struct {
 /* Quantises rows of one layer's K and V into the entries' tokens first_token[u] on, as a block's last tokens: tokens before first_token
  * in the first block that is touched keep what they stand for, rounded again under the block's new scale where that makes them
  * subnormal; the tokens behind the last row in its block become zero.  An entry is thus written front to back, in one call or in
- * many, and a write into its middle ends it there.  RELAYGR_EINVAL if two users of the batch carry the same handle. */
+ * many, and a write into its middle ends it there.  k and v must not overlap the slab.  RELAYGR_EINVAL if two users of the batch that
+ * have rows carry the same handle. */
 int  relaygr_kv_pool_write(relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, const void* k, int64_t k_stride,
                            const void* v, int64_t v_stride, void* hip_stream);
 /* The values that tokens of the entries stand for, into rows of k and v. */
@@ -298,7 +300,8 @@ int  relaygr_rank_full_recompute(relaygr_ctx* ctx, const relaygr_batch* batch,
  *   out_i^h = (1/n_i) sum_{j < n_i} SiLU(alpha <q_i^h, k_j^h>) v_j^h    or    sum_{j < n_i} softmax_j(alpha <q_i^h, k_j^h>) v_j^h,
  * alpha = 1 / sqrt(d_head), over the first n_i tokens of the user's entry: key_len[u] for every row, as candidates see a prefix, or, with
  * causal != 0, for rows that are themselves the last of these tokens: row i of the user's n sees max(0, key_len[u] - n + 1 + i).  A row that sees
- * nothing is zero.  NaN in K or V reaches the rows that see its token only.  out must not overlap q or the slab.  Uses the context's form, scratch and
+ * nothing is zero.  NaN in K or V reaches the rows that see its token only.  In fp16 the SiLU form's weights are held times
+ * log2(e), so that scores alpha <q, k> of more than 45 400 are beyond the type.  out must not overlap q or the slab.  Uses the context's form, scratch and
  * stream order (not its weights), so contexts' rules for streams, threads and graphs hold; rows are cut along the keys only as far as
  * the scratch holds their partial sums, so any call fits. */
 int  relaygr_cache_attend(relaygr_ctx* ctx, relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, int32_t causal,
@@ -310,7 +313,7 @@ int  relaygr_cache_attend(relaygr_ctx* ctx, relaygr_kv_pool* pool, int32_t layer
  * their own (0 ms, 0 launches): their work is done, and counted, in LN (SETUP) and F2 (GATE and SCORE). */
 #define RELAYGR_K_SETUP 0   /* always 0                                        */
 #define RELAYGR_K_LN    1   /* first input LayerNorm, embedding gather, row tables, tail clearing */
-#define RELAYGR_K_F1    2   /* u|v|q|k projection GEMM + SiLU + K/V scatter     */
+#define RELAYGR_K_F1    2   /* u|v|q|k projection GEMM + SiLU + K/V scatter; quantising K and V into an 8-bit pool */
 #define RELAYGR_K_ATTN  3   /* pointwise-SiLU attention over the key sequence   */
 #define RELAYGR_K_GATE  4   /* always 0                                         */
 #define RELAYGR_K_F2    5   /* layer tail: split combine, self term, 1/n, LayerNorm, gate, output projection, residual,
@@ -336,7 +339,8 @@ int  relaygr_ctx_profile_read(relaygr_ctx* ctx, int32_t kernel_class, double* to
 size_t relaygr_kv_pool_entry_bytes(relaygr_kv_pool* pool, relaygr_kv_handle handle);
 /* Enqueues on hip_stream a copy of the entry's extent into host_dst (HOST memory, pinned for an
  * asynchronous copy; host_bytes must equal relaygr_kv_pool_entry_bytes).  The entry stays live.  The
- * image is position independent: it can be reloaded into any pool of the same model shape and page size. */
+ * image is position independent: it can be reloaded into any pool of the same model shape, storage (16 or 8 bits)
+ * and page size. */
 int  relaygr_kv_pool_spill(relaygr_kv_pool* pool, relaygr_kv_handle handle, void* host_dst, size_t host_bytes,
                            void* hip_stream);
 /* Allocates an entry for user_id / prefix_len and enqueues on hip_stream the copy of a spill image

@@ -42,7 +42,7 @@ struct KvPool {
   std::vector<uint32_t> free_slots;
   std::unordered_map<uint64_t, uint32_t> by_user;
 
-  // All four return RELAYGR_* codes; these calls are thread-safe.
+  // All calls are thread-safe; these four return RELAYGR_* codes.
   int alloc(uint64_t user_id, int32_t prefix_len, relaygr_kv_handle* out);
   int release(relaygr_kv_handle h);
   int lookup(uint64_t user_id, relaygr_kv_handle* out);
