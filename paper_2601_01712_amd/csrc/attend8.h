@@ -5,6 +5,12 @@
 // and o_i = 0 where n_i = 0.  The products are those of the 16-bit kernel (attention.h): S^T = K Q^T, whose accumulator layout is the operand
 // layout of the next product, O^T += V^T P^T with P rounded to the storage type (half a step, 2^-8 or 2^-11 of each weight, signs at random); scores,
 // weights' sums and outputs are fp32.
+//
+// What bounds it: few rows, the read of the codes (128 users of one row over 8192 keys, d = 512, 1.07 GB in 161 us: 6.7 TB/s, what a read alone reaches);
+// many rows, the vector ALU, whose exp and rcp take four times as long as its other instructions (16 users of 512 rows over 4096 keys, d = 512, SiLU: 68.7
+// GFLOP in 90 us, 0.76 PFLOP/s; a 64 x 64 tile of scores is 472 vector instructions, 3424 cycles of a SIMD, and takes 3477); a single row, the launch (7.8 us).
+// Tiles come straight to registers because nothing else is gained by LDS: codes staged there and converted once for 128 or 256 rows of an item took 96 and
+// 99 us in place of 90.
 #pragma once
 
 #include "kv8.h"
@@ -220,8 +226,7 @@ __device__ __forceinline__ void attend8_join_last(const AttendParams<USERS>& p, 
 // for the same rows, each straight from memory to its registers (the codes are in operand order) with the next tile on its way while it
 // works on one; their sums meet in LDS at the end.
 //
-// ONCE: no other item reads the same codes, and the launch reads more than the caches hold: the loads do not leave them there (128 users of 8192 keys, one row
-// each, d = 512: 1.07 GB in 188 us, with the hint 167).
+// ONCE: no other item reads the same codes, and the launch reads more than the caches hold: the loads do not leave them there (attend_rules.h has both sides).
 template <typename H, int DH, int NQ, bool SOFTMAX, bool ONCE, int USERS>
 __global__ __launch_bounds__(kAttendWaves * 64, 2) void attend8_kernel(AttendParams<USERS> p) {
   constexpr int KS = DH / 16, KP = DH / 32, DB = DH / 32;

@@ -256,7 +256,7 @@ __device__ __forceinline__ void wave_lds_done() {
 
 // Writes: quantises the unit's blocks anew from the tokens before r0 that they keep and the rows of the call; tokens from r1 on become zero.
 // What bounds it is HBM, 2 bytes in and 1 out per value; loads are runs of FW * 2 bytes of a row (d = 512, 32 users of 8192 tokens, us: K in the codes' order, 32 bytes
-// of a row at a time 175, runs of 128 bytes 157).  ONCE: more than the caches hold.
+// of a row at a time 175, runs of 128 bytes 157, and 137 with nothing left in the caches: 5.9 TB/s).  ONCE: more than the caches hold.
 template <typename H, int DH, int FW, bool ONCE, int USERS>
 __global__ __launch_bounds__(256) void kv8_write_kernel(RowsParams<USERS> p) {
   using L = UnitLayout<DH, FW>;
@@ -353,7 +353,8 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(RowsParams<USERS> p) {
   }
 }
 
-// Reads: the values that the unit's tokens [r0, r1) stand for, into their rows; 1 byte in and 2 out per value.
+// Reads: the values that the unit's tokens [r0, r1) stand for, into their rows; 1 byte in and 2 out per value (32 users of 8192 tokens, d = 512: 806 MB in 148 us,
+// 5.4 TB/s; one user of 1001 tokens, 6.2 MB, 8.8, which is the launch).
 template <typename H, int DH, int FW, bool ONCE, int USERS>
 __global__ __launch_bounds__(256) void kv8_read_kernel(RowsParams<USERS> p) {
   using L = UnitLayout<DH, FW>;
