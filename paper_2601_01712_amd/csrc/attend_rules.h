@@ -28,7 +28,7 @@ inline int attend_parts(int nk, int piece) {
 
 // Whether a launch of few users joins the pieces of its rows itself, the last workgroup of an item's to arrive, or leaves that to a second launch, which takes 3.3 us of
 // the host and 2 of the GPU but has all of the chip for it.  most_sums: rows of an item times its pieces, at most.
-// (us among calls, itself / a second launch: one row over 2048 keys 7.8 / 10.4; in launches of many users, whose kernels do without it, the wait for the sums to reach
+// (us among calls, itself / a second launch: one row over 2048 keys 8.2 / 11.0; in launches of many users, whose kernels do without it, the wait for the sums to reach
 // the other XCDs costs more than the launch: 32 users of 8 to 60 rows over about 4096 keys 41.7 / 38.9.)
 inline bool attend_joins_itself(int most_sums, int64_t items, int counters) { return most_sums <= 256 && items <= counters; }
 
