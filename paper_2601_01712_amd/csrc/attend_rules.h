@@ -42,7 +42,10 @@ inline bool attend_joins_itself(int most_sums, int64_t items, int counters) { re
 // Sequences are cut where the launch has fewer items than the chip has compute units (at d = 512 one user of 4096 keys: 512 rows, 128 items, uncut 16.1, 256
 // pieces 13.4, 512 14.8; one row of 16 384 keys, 8 items, uncut 50, 128 pieces 10.4, 256 11.2, 512 14.4), and where items are of unequal length
 // those that would be left running behind the others (32 users of 8 to 60 rows over about 4096 keys, 48 key tiles a piece 40.6, uncut 55.6): each cut
-// is a partial sum to write and read and the first one a launch.  448 equal items of 33 tiles: uncut 12.3, in halves 14.5.
+// is a partial sum to write and read and the first one a launch.  Unequal items: as many pieces as the chip has room for at once, so that no compute unit is left with the
+// last; three a unit (d_head 128 and two blocks: the registers hold two), unless these are short.  us, pieces for two a unit / for three: the 32 users above 35.6 / 32.9, 24
+// of 1 to 8 rows over about 6000 40.3 / 35.0, 50 of 30 to 64, causal, 71 / 65, 8 of 100 to 300 over 3000 42.5 / 38.4; fewer keys: 100 of 1 to 4 rows over about
+// 1000 (16 784 key tiles) 29.5 / 30.7, 6 of 4 to 40 over about 10 000 (10 096) 18.9 / 20.0; d_head 128 in 12 of 20 to 90 over about 5000 47.9 / 50.0.  448 equal items of 33 tiles: uncut 12.3, in halves 14.5.
 //
 // Codes that one item alone reads, more of them than the caches could keep until they are read again: 128 users of 8192 keys, one row each (1.07 GB) 180 / 162
 // without keeping, of 2048 and four rows (268 MB) 51.3 / 44.8; 64 of 4096 and 20 at d = 1024 93.7 / 83.4.
@@ -65,7 +68,7 @@ inline AttendRule attend_rule(const std::vector<AttendLen>& users, int heads, in
   for (const AttendLen& u : users) key_tiles += (u.rows + 32 * r.blocks - 1) / (32 * r.blocks) * (int64_t)((u.keys + kTile - 1) / kTile) * heads;
   const bool equal = 3 * most * items <= 4 * key_tiles;                   // the longest is at most a third over the mean
   if (equal && items >= n_cus) return r;
-  const int64_t slots = equal ? n_cus : 2 * n_cus;
+  const int64_t slots = equal ? n_cus : dh < 128 && r.blocks == 1 && key_tiles >= 80 * (int64_t)n_cus ? 3 * n_cus : 2 * n_cus;
   r.piece = (int)std::max<int64_t>(kLeastPiece, std::min<int64_t>((key_tiles + slots - 1) / slots, 1 << 20));
   return r;
 }
