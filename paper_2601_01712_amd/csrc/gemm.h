@@ -20,6 +20,7 @@ typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 // of two 8-element fragments (any 16-byte type), mfma16 the 16x16x32 one.
 struct Bf16 {
   using elem = __hip_bfloat16;
+  static constexpr uint32_t kOnes = 0x3F803F80u;      // a pair of ones
   static __device__ __forceinline__ float to_f32(uint16_t b) { return __uint_as_float(((uint32_t)b) << 16); }
   static __device__ __forceinline__ float of_word(uint32_t w, int i) { return __uint_as_float((i & 1) ? (w & 0xFFFF0000u) : (w << 16)); }
   static __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -41,6 +42,7 @@ struct Bf16 {
 };
 struct F16 {
   using elem = __half;
+  static constexpr uint32_t kOnes = 0x3C003C00u;
   static __device__ __forceinline__ float to_f32(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
   static __device__ __forceinline__ float of_word(uint32_t w, int i) { return (float)__builtin_bit_cast(f16x2_t, w)[i & 1]; }
   static __device__ __forceinline__ uint32_t pack2(float a, float b) {
