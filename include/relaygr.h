@@ -300,11 +300,11 @@ int  relaygr_rank_full_recompute(relaygr_ctx* ctx, const relaygr_batch* batch,
  *   out_i^h = (1/n_i) sum_{j < n_i} SiLU(alpha <q_i^h, k_j^h>) v_j^h    or    sum_{j < n_i} softmax_j(alpha <q_i^h, k_j^h>) v_j^h,
  * alpha = 1 / sqrt(d_head), over the first n_i tokens of the user's entry: key_len[u] for every row, as candidates see a prefix, or, with
  * causal != 0, for rows that are themselves the last of these tokens: row i of the user's n sees max(0, key_len[u] - n + 1 + i).  A row that sees
- * nothing is zero.  Each weight is rounded to the storage type before it is multiplied with V (softmax: and before it is added to their sum), scores and sums
- * are fp32.  NaN in K or V reaches the rows that see its token only.  In fp16 the SiLU form's weights are held times
- * log2(e), so that scores alpha <q, k> of more than 45 400 are beyond the type.  out must not overlap q or the slab.  Uses the context's form, scratch and
- * stream order (not its weights), so contexts' rules for streams, threads and graphs hold; rows are cut along the keys only as far as
- * the scratch holds their partial sums, so any call fits. */
+ * nothing is zero.  Each weight is rounded to the storage type before it is multiplied with V (softmax: and before it is added to their sum), scores and
+ * sums are fp32.  NaN in K or V reaches the rows that see its token only.  In fp16 the SiLU form's weights are held times log2(e), so that scores alpha
+ * <q, k> of more than 45 400 are beyond the type.  out must not overlap q or the slab.  The pool's slab, the context's scratch and the stream are one
+ * device's.  Uses the context's form, scratch and stream order (not its weights), so contexts' rules for streams, threads and graphs hold; rows are cut
+ * along the keys only as far as the scratch holds their partial sums, so any call fits. */
 int  relaygr_cache_attend(relaygr_ctx* ctx, relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, int32_t causal,
                           const void* q, int64_t q_stride, void* out, int64_t out_stride, void* hip_stream);
 

@@ -451,6 +451,8 @@ def relaygr_kv_pool_read(pool: KvPool, layer: int, rows: KvRows, k: Optional[tor
 def relaygr_cache_attend(ctx: Context, pool: KvPool, layer: int, rows: KvRows, q: torch.Tensor, causal: bool = False,
                          out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """One layer's attention of query rows over entries of an 8-bit pool, in the context's form: [rows, d_model] (made here if not given)."""
+    if ctx.scratch.device != pool.slab.device:
+        raise RelayGRError(RELAYGR_EINVAL, f"cache_attend: a context on {ctx.scratch.device} for a pool on {pool.slab.device}")
     guard = _kv_guard(pool, stream)
     if guard is not None:
         with guard:
