@@ -366,7 +366,8 @@ class KvRows:
     """The host arrays of a relaygr_kv_rows: which rows of a call's tensors belong to which entry, and where in it they are.
 
     row_off: n_users + 1 offsets.  first_token (write, read): token of the entry that a user's first row is; None: 0.  key_len
-    (attend): tokens of the entry that take part; None: all.  Made once, used in any number of calls."""
+    (attend): tokens of the entry that take part; None: all.  Made once, used in any number of calls, between which handles, first_token and
+    key_len may be changed in place; row_off, which the checks of the calls' tensors go by, and which array is which are fixed."""
 
     def __init__(self, handles: Sequence[int], row_off: Sequence[int], first_token: Optional[Sequence[int]] = None,
                  key_len: Optional[Sequence[int]] = None):
@@ -380,12 +381,18 @@ class KvRows:
             if a is not None and a.shape != (n,):
                 raise RelayGRError(RELAYGR_EINVAL, f"KvRows: {name} has shape {a.shape}, ({n},) is needed")
         self.n_rows = int(self.row_off[-1])
+        self.row_off.flags.writeable = False
 
         def ptr(a):
             return None if a is None else a.ctypes.data_as(C.POINTER(C.c_int32))
         self.c = KvRowsC(self.n_users, self.handles.ctypes.data_as(C.POINTER(C.c_uint64)), ptr(self.row_off), ptr(self.first_token),
                          ptr(self.key_len))
         self.ref = C.byref(self.c)
+
+    def __setattr__(self, name, value):
+        if "ref" in self.__dict__ and value is not self.__dict__.get(name):     # (made: the library has the arrays' addresses; a += puts the same one back)
+            raise AttributeError(f"KvRows: {name} cannot be replaced; change handles, first_token and key_len in place, or make another")
+        object.__setattr__(self, name, value)
 
 
 def _kv_rows_array(what: str, pool: KvPool, rows: KvRows, t: torch.Tensor):

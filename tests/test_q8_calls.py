@@ -14,3 +14,19 @@ def test_attention_refuses_a_context_on_another_device_than_the_pool():
     with pytest.raises(rg.RelayGRError) as e:
         rg.relaygr_cache_attend(ctx, pool, 0, rg.KvRows([1], [0, 1]), torch.zeros(1, 256, dtype=torch.bfloat16))
     assert e.value.code == rg.RELAYGR_EINVAL and "context on meta" in str(e.value)
+
+
+def test_rows_keep_their_offsets_and_take_other_values_in_place():
+    """The library reads a KvRows' arrays where they are; the binding checks tensors by their last offset, which therefore stays."""
+    rows = rg.KvRows([5, 6], [0, 1, 3], first_token=[10, 20], key_len=[11, 22])
+    with pytest.raises(ValueError):
+        rows.row_off[-1] = 100
+    for name, value in (("row_off", rows.row_off.copy()), ("n_rows", 100), ("n_users", 1), ("handles", rows.handles.copy()), ("first_token", None),
+                        ("key_len", rows.key_len + 1)):
+        with pytest.raises(AttributeError):
+            setattr(rows, name, value)
+    assert rows.n_rows == rows.c.row_off[2] == 3
+    rows.first_token += 1
+    rows.key_len[1] = 23
+    rows.handles[0] = 7
+    assert [rows.c.first_token[i] for i in range(2)] == [11, 21] and rows.c.key_len[1] == 23 and rows.c.handles[0] == 7
