@@ -35,9 +35,9 @@ int resolve_rows(const char* what, KvPool* pool, int32_t layer, const relaygr_kv
   if (!pool->q8) return fail(RELAYGR_EINVAL, "%s: the pool does not hold 8-bit K/V", what);
   if (layer < 0 || layer >= pool->cfg.n_layers) return fail(RELAYGR_EINVAL, "%s: layer %d out of range", what, layer);
   if (r->n_users < 0) return fail(RELAYGR_EINVAL, "%s: n_users < 0", what);
+  if (r->row_off && r->row_off[0] != 0) return fail(RELAYGR_EINVAL, "%s: row offsets must start at 0", what);
   if (r->n_users == 0) return RELAYGR_OK;
   if (!r->handles || !r->row_off) return fail(RELAYGR_EINVAL, "%s: null handles or row offsets", what);
-  if (r->row_off[0] != 0) return fail(RELAYGR_EINVAL, "%s: row offsets must start at 0", what);
   for (int u = 0; u < r->n_users; ++u)
     if (r->row_off[u + 1] < r->row_off[u]) return fail(RELAYGR_EINVAL, "%s: row offsets not monotone at user %d", what, u);
   entries->resize(r->n_users);

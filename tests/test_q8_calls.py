@@ -1,4 +1,5 @@
 """Calls of the 8-bit cache that are refused, or that arrays changed between calls reach, without a GPU: nothing here gets as far as a launch."""
+import ctypes as C
 import types
 
 import pytest
@@ -30,3 +31,21 @@ def test_rows_keep_their_offsets_and_take_other_values_in_place():
     rows.key_len[1] = 23
     rows.handles[0] = 7
     assert [rows.c.first_token[i] for i in range(2)] == [11, 21] and rows.c.key_len[1] == 23 and rows.c.handles[0] == 7
+
+
+@pytest.mark.parametrize("name", ["relaygr_kv_pool_write", "relaygr_kv_pool_read"])
+def test_rows_that_belong_to_no_user_are_refused(name):
+    """Offsets start at 0 with no users too: rows before the first user would be returned as nobody wrote them."""
+    lib, cfg, handle = rg.load_library(), rg.make_config(2, 256, 4, "bf16"), C.c_void_p()
+    assert lib.relaygr_kv_pool_create_q8(C.byref(cfg), C.c_void_p(0x10000000), 1 << 24, 64, C.byref(handle)) == 0
+
+    def call(row_off):
+        rows = rg.KvRows([], row_off)
+        return getattr(lib, name)(handle, 0, rows.ref, 0x1000, 256, 0x2000, 256, None)
+    try:
+        assert call([5]) == rg.RELAYGR_EINVAL and "start at 0" in rg.relaygr_last_error()
+        assert call([0]) == 0
+        none = rg.binding.KvRowsC()
+        assert getattr(lib, name)(handle, 0, C.byref(none), None, 256, None, 256, None) == 0
+    finally:
+        lib.relaygr_kv_pool_destroy(handle)
