@@ -32,6 +32,11 @@ inline int attend_parts(int nk, int piece) {
 // the other XCDs costs more than the launch: 32 users of 8 to 60 rows over about 4096 keys 41.7 / 38.9.)
 inline bool attend_joins_itself(int most_sums, int64_t items, int counters) { return most_sums <= 256 && items <= counters; }
 
+// Workgroups of a launch of `items` items for each head, heads dealt to eight XCDs; and whether a launch takes them: it counts its threads, 256 a workgroup,
+// in 32 bits.
+inline int64_t attend_groups(int64_t items, int heads) { return heads >= 8 ? items * heads : (items + 8 / heads - 1) / (8 / heads) * 8; }
+inline bool attend_fits(int64_t items, int heads) { return attend_groups(items, heads) < 1ll << 24; }
+
 // A workgroup is four wavefronts that share an item's key tiles, and two or three of them a compute unit are full speed.
 //
 // Two blocks of 32 rows an item (one conversion of the codes for twice the rows) where the launch still has four items a compute unit and users have

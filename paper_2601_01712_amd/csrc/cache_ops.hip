@@ -130,8 +130,7 @@ int move_rows(const char* what, KvPool* pool, int32_t layer, const relaygr_kv_ro
 
 template <typename H, int DH, bool SM, int USERS>
 void launch_attend(const AttendParams<USERS>& p, int blocks, bool once, hipStream_t st) {
-  const int nh = p.n_heads;
-  const dim3 grid(nh >= 8 ? p.n_items * nh : (p.n_items + 8 / nh - 1) / (8 / nh) * 8), block(kAttendWaves * 64);
+  const dim3 grid((unsigned)attend_groups(p.n_items, p.n_heads)), block(kAttendWaves * 64);
   if constexpr (USERS > kFewAttendUsers) {
     if constexpr (DH == 64) {
       if (blocks == 2) { hipLaunchKernelGGL((attend8_kernel<H, DH, 2, SM, false, USERS>), grid, block, 0, st, p); return; }
@@ -189,10 +188,11 @@ int relaygr::attend8(KvPool* pool, const AttendCall& c, hipStream_t st) {
   const int blocks = rule.blocks, item_rows = 32 * blocks;
   const bool once = rule.once;
   const size_t row_bytes = (size_t)d * 4 + (c.softmax ? (size_t)H * 8 : 0);
-  int64_t partial_rows;
+  const auto items_of = [&](const Work& w) { return ((int64_t)w.rows + item_rows - 1) / item_rows * w.parts; };
+  int64_t partial_rows, most_items;
   int most_sums;      // rows of an item times its pieces
   for (;; rule.piece = rule.piece > 1 << 20 ? 0 : 2 * rule.piece) {      // (0: nothing is cut)
-    partial_rows = 0;
+    partial_rows = most_items = 0;
     most_sums = 0;
     for (Work& w : work) {
       const int nk = (w.keys + kTile - 1) / kTile;
@@ -200,9 +200,11 @@ int relaygr::attend8(KvPool* pool, const AttendCall& c, hipStream_t st) {
       w.per = std::max(1, (nk + w.parts - 1) / w.parts);
       if (w.parts > 1) partial_rows += (int64_t)w.parts * w.rows;
       most_sums = std::max(most_sums, std::min(w.rows, item_rows) * w.parts);
+      most_items = std::max(most_items, items_of(w));
     }
-    if (partial_rows == 0 || ((size_t)partial_rows * row_bytes <= c.scratch_bytes && partial_rows < (1ll << 31))) break;
+    if (partial_rows == 0 || ((size_t)partial_rows * row_bytes <= c.scratch_bytes && partial_rows < (1ll << 31) && attend_fits(most_items, H))) break;
   }
+  if (!attend_fits(most_items, H)) return fail(RELAYGR_EINVAL, "%s: %lld row tiles of one user are more than a launch takes", what, (long long)most_items);
   std::stable_sort(work.begin(), work.end(), [](const Work& a, const Work& b) { return a.per > b.per; });    // the longest pieces first
 
   (void)hipGetLastError();
@@ -224,9 +226,10 @@ int relaygr::attend8(KvPool* pool, const AttendCall& c, hipStream_t st) {
       p.n_users = 0; p.n_items = 0; j.n_users = 0; j.n_rows = 0;
       for (; i < work.size() && p.n_users < USERS; ++i) {
         const Work& w = work[i];
+        if (!attend_fits(p.n_items + items_of(w), H)) break;      // (never a launch's first)
         const int32_t row0 = r->row_off[w.user];
         p.users[p.n_users++] = {(int32_t)entries[w.user].page0, row0, w.rows, w.keys, p.n_items, part0, (uint32_t)w.parts | (uint32_t)w.per << 7};
-        p.n_items += (w.rows + item_rows - 1) / item_rows * w.parts;
+        p.n_items += (int32_t)items_of(w);
         if (w.parts == 1) continue;
         j.users[j.n_users++] = {row0, w.rows, w.keys, part0, w.parts, j.n_rows};
         j.n_rows += w.rows;

@@ -1,5 +1,8 @@
 """Calls of the 8-bit cache that are refused, or that arrays changed between calls reach, without a GPU: nothing here gets as far as a launch."""
 import ctypes as C
+import os
+import shutil
+import subprocess
 import types
 
 import pytest
@@ -49,3 +52,21 @@ def test_rows_that_belong_to_no_user_are_refused(name):
         assert getattr(lib, name)(handle, 0, C.byref(none), None, 256, None, 256, None) == 0
     finally:
         lib.relaygr_kv_pool_destroy(handle)
+
+
+def test_launches_count_their_threads_in_32_bits(tmp_path):
+    """Workgroups of 256 threads: one for each item and head, in eights where an XCD has no head of its own."""
+    if shutil.which("g++") is None:
+        pytest.skip("no g++")
+    lib, src = tmp_path / "attend_launch.so", os.path.join(os.path.dirname(os.path.abspath(__file__)), "attend_launch_shim.cpp")
+    subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-Wextra", "-Werror", "-shared", "-fPIC", src, "-o", str(lib)], check=True)
+    shim = C.CDLL(str(lib))
+    shim.attend_groups_of.argtypes, shim.attend_groups_of.restype = [C.c_int64, C.c_int], C.c_int64
+    shim.attend_fits_in.argtypes = [C.c_int64, C.c_int]
+    for heads in (1, 2, 4, 8, 16, 32):
+        for items in (1, 2, 7, 8, 9, 1000, (1 << 24) // heads - 8, (1 << 24) // heads, (1 << 31) // 32, 1 << 40):
+            groups = shim.attend_groups_of(items, heads)
+            assert groups >= items * heads and groups % min(8, max(heads, 8)) == 0 and groups - items * heads < 8
+            assert bool(shim.attend_fits_in(items, heads)) == (groups * 256 < 1 << 32)
+        # 32 rows an item: fewer than 2^29 / heads rows of one user fit uncut, save for the last few items
+        assert shim.attend_fits_in((1 << 24) // heads - 8, heads) and not shim.attend_fits_in((1 << 24) // heads, heads)
