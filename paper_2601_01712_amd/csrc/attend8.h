@@ -10,11 +10,13 @@
 // alone 0.0017.  fp16: an eighth of that).  The rest of the weights in a product of its own would be half of the MFMAs again.  The softmax form's sums are of the rounded
 // weights, so that a row is a mean of V whatever they round to: a weight that is most of its row's rounds in the numerator and in the denominator.
 //
-// What bounds it: few rows, the read of the codes (128 users of one row over 8192 keys, d = 512, 1.07 GB in 161 us: 6.7 TB/s, what a read alone reaches);
-// many rows, the vector ALU, whose exp and rcp take four times as long as its other instructions (16 users of 512 rows over 4096 keys, d = 512, SiLU: 68.7
-// GFLOP in 90 us, 0.76 PFLOP/s; a 64 x 64 tile of scores is 472 vector instructions, 3424 cycles of a SIMD, and takes 3477); a single row, the launch (7.8 us).
+// What bounds it: few rows, the read of the codes (128 users of one row over 8192 keys, d = 512, 1.07 GB in 161 us: 6.7 TB/s, where a kernel that reads 1 to 4 GiB
+// and does nothing else reaches 6.9 to 7.1); many rows, the vector ALU (16 users of 512 rows over 4096 keys, d = 512, SiLU: 68.7 GFLOP in 88 to 94 us by the card, 0.73
+// to 0.78 PFLOP/s).  A 64 x 64 tile of scores is 472 vector instructions there, 128 of them exp and rcp; by the counters they issue for 2402 cycles of a SIMD, 4 an instruction
+// and 8 an exp or rcp, 79 % of the 3034 that its compute unit is busy for it (the MFMAs' 1024 beside them; 1.77 wavefronts a SIMD of 2 in the mean, the others starting or
+// done, 12 % of their time at waits).  A single row: the launch (7.9 us a call, 6.0 of them on the GPU).
 // Tiles come straight to registers because nothing else is gained by LDS: codes staged there and converted once for 128 or 256 rows of an item took 96 and
-// 99 us in place of 90.
+// 99 us where this took 88.
 #pragma once
 
 #include "kv8.h"

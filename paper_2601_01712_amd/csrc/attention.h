@@ -225,7 +225,7 @@ __device__ __forceinline__ void softmax_track(const f32x16_t (&s)[NQ], const int
 // tile, and turns it into the 16-bit tile's LDS image, which holds exactly what the codes stand for, when the ring slot becomes free.  Half the bytes of K/V
 // for 1/NW of a tile's conversions per wavefront (dh = 64, four wavefronts: 16 instructions and four LDS stores), which are in the way of wavefronts that
 // have their SIMD to themselves and of no weight where two share it.  us a ranking on a 16-bit / on an 8-bit pool, d = 512, 8 layers: 128 users of 8192 keys and 32
-// candidates 3256 / 2845, of one 2999 / 2745; 16 of 4096 and 512 1006 / 1005; one of 4096 and 512 232 / 249.
+// candidates 3256 / 2845 (on another card 3257 / 2990), of one 2999 / 2745; 16 of 4096 and 512 1006 / 1005 (1084 / 1103); one of 4096 and 512 232 / 249.
 template <typename H, int DH, int NQ, int NW, bool SOFTMAX, int GS = 1, bool Q8 = false>
 __global__ __launch_bounds__(NW * GS * 64, (DH >= 128 || GS > 1) ? 1 : 512 / (NW * 64)) void attn_bf16_kernel(AttnParams p) {   // DH = 128: the 96 KiB tile ring admits one workgroup per compute unit
   constexpr int KS = DH / 16;              // k-steps of the first product
