@@ -41,7 +41,8 @@ inline bool attend_fits(int64_t items, int heads) { return attend_groups(items, 
 //
 // Two blocks of 32 rows an item (one conversion of the codes for twice the rows) where the launch still has four items a compute unit and users have
 // so many rows that few blocks are empty; at d_head 64, where the registers hold them.  us, one block / two, d = 512: 16 users of 512 rows over 4096
-// keys 94.4 / 88.1, 32 of 200 to 1000 over about 4096 249 / 238; fewer items: one of 512 over 4096 13.4 / 15.4; few rows: 64 of 50 to 100 103 / 120; d_head 32, 16
+// keys 94.4 / 88.1, 32 of 200 to 1000 over about 4096 249 / 238, softmax 87.8 / 83.2 and 228 / 215; 64 of 200 over 2048, whose fourth block of 64 is nearly empty,
+// 95.9 / 103, softmax 85.8 / 91.8, 40 of 200 to 700, causal, over about 1500 76.7 / 77.7; fewer items: one of 512 over 4096 13.4 / 15.4; few rows: 64 of 50 to 100 103 / 120; d_head 32, 16
 // of 500 to 1000 over 8000 211 / 218.
 //
 // Sequences are cut where the launch has fewer items than the chip has compute units (at d = 512 one user of 4096 keys: 512 rows, 128 items, uncut 16.1, 256
