@@ -52,7 +52,7 @@ inline bool attend_fits(int64_t items, int heads) { return attend_groups(items, 
 // last; three a unit (d_head 128 and two blocks: the registers hold two), unless these are short.  us, pieces for two a unit / for three: the 32 users above 35.6 / 32.9, 24
 // of 1 to 8 rows over about 6000 40.3 / 35.0, 50 of 30 to 64, causal, 71 / 65, 8 of 100 to 300 over 3000 42.5 / 38.4; fewer keys: 100 of 1 to 4 rows over about
 // 1000 (16 784 key tiles) 29.5 / 30.7, 6 of 4 to 40 over about 10 000 (10 096) 18.9 / 20.0; d_head 128 in 12 of 20 to 90 over about 5000 47.9 / 50.0.  Around the
-// switch single lists decide more than their size: 22 lists at d_head 64 and 22 at 32, of 38 to 145 key tiles a unit (12 to 48 users of 1 to 90 rows), three over two 0.87 to 1.12; mean of those with 80
+// switch single lists decide more than their size: 22 lists at d_head 64 and 22 at 32, of 38 to 145 key tiles a unit (12 to 48 users of 1 to 90 rows), three over two 0.88 to 1.12; mean of those with 80
 // and more 0.98 at either d_head, of those with 53 to 80 0.97 too, of those with 38 1.03.  448 equal items of 33 tiles: uncut 12.3, in halves 14.5.
 //
 // Codes that one item alone reads, more of them than the caches could keep until they are read again: 128 users of 8192 keys, one row each (1.07 GB) 180 / 162
