@@ -304,7 +304,8 @@ int  relaygr_rank_full_recompute(relaygr_ctx* ctx, const relaygr_batch* batch,
  * sums are fp32.  NaN in K or V reaches the rows that see its token only.  In fp16 the SiLU form's weights are held times log2(e), so that scores alpha
  * <q, k> of more than 45 400 are beyond the type.  out must not overlap q or the slab.  The pool's slab, the context's scratch and the stream are one
  * device's.  Uses the context's form, scratch and stream order (not its weights), so contexts' rules for streams, threads and graphs hold; rows are cut
- * along the keys only as far as the scratch holds their partial sums, so any call fits whose users have at most 2^29 / n_heads - 256 rows each (RELAYGR_EINVAL beyond 2^29 / n_heads). */
+ * along the keys only as far as the scratch holds their partial sums, so any call fits whose users have at most 2^29 / n_heads - 256 rows each
+ * (RELAYGR_EINVAL for a user of more than a launch takes). */
 int  relaygr_cache_attend(relaygr_ctx* ctx, relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, int32_t causal,
                           const void* q, int64_t q_stride, void* out, int64_t out_stride, void* hip_stream);
 

@@ -235,7 +235,7 @@ int relaygr::attend8(KvPool* pool, const AttendCall& c, hipStream_t st) {
         j.n_rows += w.rows;
         part0 += w.parts * w.rows;
       }
-      if (USERS == kFewAttendUsers && c.arrived && attend_joins_itself(most_sums, (int64_t)p.n_items * H, kArrivals)) p.arrived = c.arrived;
+      p.arrived = USERS == kFewAttendUsers && attend_joins_itself(most_sums, (int64_t)p.n_items * H, kArrivals) ? c.arrived : nullptr;
       by_head(cfg, [&](auto h, auto dim) {
         using HT = decltype(h);
         constexpr int DH = decltype(dim)::value;
