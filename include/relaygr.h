@@ -309,6 +309,78 @@ int  relaygr_rank_full_recompute(relaygr_ctx* ctx, const relaygr_batch* batch,
 int  relaygr_cache_attend(relaygr_ctx* ctx, relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, int32_t causal,
                           const void* q, int64_t q_stride, void* out, int64_t out_stride, void* hip_stream);
 
+/* ---- positions, scores, masks and eviction, for backbones that bring their own projections ---------------------------------------------------- */
+
+/* Rotary positions.  Pair i of the first `dim` features of a head turns by position * f_i, f_i = base^(-2 i / dim); a `factor` stretches the
+ * positions that a model was made for: f_i (r + (1 - r) / factor), with r = 0 (original_len = 0: every pair is stretched), or r = clamp((n_i - low) /
+ * (high - low), 0, 1), n_i = original_len f_i / 2 pi the pair's turns in original_len positions (pairs that turn often keep their frequency). */
+#define RELAYGR_ROPE_HALF        0   /* pairs (i, i + dim / 2) */
+#define RELAYGR_ROPE_INTERLEAVED 1   /* pairs (2 i, 2 i + 1)   */
+typedef struct {
+  int32_t  dim, layout;
+  float    gain;              /* what turned features are multiplied with: 1, or the sharpening of scores over more tokens */
+  int32_t  reserved;
+  uint64_t turns[64];         /* of pair i: the fraction of a turn per position, times 2^64 (a caller may set frequencies of its own) */
+} relaygr_rope;
+/* Fills *out.  RELAYGR_EINVAL for a dim that is not even and between 2 and 128, an unknown layout, a base or factor that is not positive and finite, or
+ * original_len > 0 without low < high. */
+int  relaygr_rope_init(relaygr_rope* out, int32_t dim, int32_t layout, double base, double factor, int32_t original_len, double low, double high, float gain);
+/* Turns rows of q, and of k unless it is null, by the rows' positions (DEVICE int32 [n_rows]; any value, negative ones too): a' = gain (a cos - b sin),
+ * b' = gain (a sin + b cos), the head's features from `dim` on copied; transposed != 0: by the opposite angle, which is the gradient of that, and undoes it where gain
+ * is 1.  Arrays as in the calls on an 8-bit pool, in cfg's storage type, fp32 too (rows 16-byte aligned: strides a multiple of 4 elements there);
+ * angles and products are fp32 or better at any position, results are rounded once.  q_out may be q with the same stride, k_out k; other overlaps
+ * are not allowed.  No context, no scratch: it may be captured, and calls on different rows may run at once. */
+int  relaygr_rotary(const relaygr_model_config* cfg, const relaygr_rope* rope, int32_t n_rows, const int32_t* positions, int32_t transposed,
+                    const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, void* k_out,
+                    int64_t k_out_stride, void* hip_stream);
+
+/* Scores and masks of relaygr_cache_attend_scored.  All zero: as relaygr_cache_attend.  With t_ij = alpha <q_i, k_j>,
+ *   cap > 0:   t_ij <- cap tanh(t_ij / cap)
+ *   slopes:    t_ij <- t_ij - slopes[h] |p_i - p_j|, p_j the token's place in the entry, p_i = key_len, or key_len - n + i for row i of n causal ones; or as
+ *              row_position and key_position say (differences have to fit 32 bits)
+ * and row i sees the first prefix[u] tokens, whatever else holds, and those in [first_i, end_i): end_i = key_len, causal rows key_len - n + 1 + i, and no more than
+ * row_end[i]; first_i = 0, no less than row_first[i] (a session, a document), and no less than end_i - window if window > 0. */
+typedef struct {
+  float cap;                     /* 0: none */
+  int32_t window;                /* 0: none */
+  const float* slopes;           /* DEVICE [n_heads], or null: no bias */
+  const int32_t* prefix;         /* HOST [n_users], or null: 0 (more than key_len counts as key_len) */
+  const int32_t* row_first;      /* DEVICE [rows], or null */
+  const int32_t* row_end;        /* DEVICE [rows], or null */
+  const int32_t* row_position;   /* DEVICE [rows], or null */
+  const int32_t* key_position;   /* DEVICE, or null: of token j of user u at [token_off[u] + j] */
+  const int64_t* token_off;      /* HOST [n_users]; null if neither key_position nor weights are given */
+} relaygr_scoring;
+/* One layer's attention over entries of an 8-bit pool with such scores and masks, otherwise as relaygr_cache_attend (arrays, forms, roundings, errors; n_i counts
+ * the tokens that row i sees; rows that see nothing are zero).  weight_out (DEVICE fp32, or null): what each token received, added up,
+ *   weight_out[token_off[u] + j] = weight_in[token_off[u] + j] + sum over heads and rows of w_ij      (|w_ij| in the SiLU form; weight_in null: from 0)
+ * for the first key_len[u] tokens of every user, in fp32 and in an order that the call's sizes and the context's scratch decide; weight_in may be weight_out.
+ * RELAYGR_EINVAL if two users' tokens overlap there.  RELAYGR_ENOSPC if the scratch does not hold 4 n_heads bytes a row (softmax with weights). */
+int  relaygr_cache_attend_scored(relaygr_ctx* ctx, relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, int32_t causal,
+                                 const relaygr_scoring* scoring, const void* q, int64_t q_stride, void* out, int64_t out_stride,
+                                 const float* weight_in, float* weight_out, void* hip_stream);
+
+/* Which tokens stay in relaygr_kv_pool_evict. */
+typedef struct {
+  int32_t first, recent;         /* tokens at an entry's front and end that stay whatever their weight */
+  const relaygr_kv_handle* to;   /* HOST [n_users] entries that take what stays; null: in place */
+  const float* weight;           /* DEVICE: of token j of user u at [token_off[u] + j] */
+  const int32_t* position;       /* DEVICE, laid out like weight, or null */
+  const int64_t* token_off;      /* HOST [n_users] */
+  int32_t* kept;                 /* DEVICE [rows]: places of the tokens that stay, climbing, from row_off[u] on */
+  float* weight_out;             /* DEVICE, or null: weights of the tokens that stay, from [out_off[u]] on */
+  int32_t* position_out;         /* DEVICE, or null: positions of the tokens that stay */
+  const int64_t* out_off;        /* HOST [n_users], or null: row_off */
+} relaygr_kv_eviction;
+/* Evicts the tokens that were attended to least: of the first key_len[u] tokens of the entry, row_off[u+1] - row_off[u] stay (the rows of the batch are what
+ * stays): the `first` ones, the `recent` last ones, and of the others those with the largest weight, ties going to the lowest place; NaN is below every
+ * number.  They become the first tokens of the entry, or of to[u], in their order and in every layer, quantised anew from the values their codes stand for; the tokens behind
+ * them in their last block become zero, and an entry of which nothing stays is left as it is.  A token keeps the position its K was made for: pass on `position`.  weight_out may be weight,
+ * and position_out position, with out_off = token_off; outputs must not overlap otherwise.  No context, no scratch: it may be captured.  Errors as in the calls on an 8-bit pool;
+ * RELAYGR_EINVAL also if more tokens are to stay than there are or than to[u] holds, if first + recent are more than that where any leave, and if an entry
+ * would be written twice or written by one user and read by another. */
+int  relaygr_kv_pool_evict(relaygr_kv_pool* pool, const relaygr_kv_rows* rows, const relaygr_kv_eviction* eviction, void* hip_stream);
+
 /* ---- measurement ---------------------------------------------------------------------- */
 
 /* Kernel classes of the layer sequence, for per-kernel timing.  SETUP, GATE and SCORE have no launches of

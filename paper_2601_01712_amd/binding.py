@@ -39,6 +39,7 @@ EXPORTS = [
     "relaygr_trigger_stats",
     "relaygr_kv_footprint_bytes_q8", "relaygr_kv_pool_bytes_for_q8", "relaygr_kv_pool_create_q8",
     "relaygr_kv_pool_write", "relaygr_kv_pool_read", "relaygr_cache_attend",
+    "relaygr_rope_init", "relaygr_rotary", "relaygr_cache_attend_scored", "relaygr_kv_pool_evict",
     "relaygr_last_error",
 ]
 EXPANDER_STATS = ["hbm_hits", "dram_hits", "misses", "refusals", "spills", "dram_evictions", "dram_bytes", "dram_entries",
@@ -73,6 +74,21 @@ class BatchC(C.Structure):
 class KvRowsC(C.Structure):
     _fields_ = [("n_users", C.c_int32), ("handles", C.POINTER(C.c_uint64)), ("row_off", C.POINTER(C.c_int32)),
                 ("first_token", C.POINTER(C.c_int32)), ("key_len", C.POINTER(C.c_int32))]
+
+
+class RopeC(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("layout", C.c_int32), ("gain", C.c_float), ("reserved", C.c_int32), ("turns", C.c_uint64 * 64)]
+
+
+class ScoringC(C.Structure):
+    _fields_ = [("cap", C.c_float), ("window", C.c_int32), ("slopes", C.c_void_p), ("prefix", C.POINTER(C.c_int32)), ("row_first", C.c_void_p),
+                ("row_end", C.c_void_p), ("row_position", C.c_void_p), ("key_position", C.c_void_p), ("token_off", C.POINTER(C.c_int64))]
+
+
+class KvEvictionC(C.Structure):
+    _fields_ = [("first", C.c_int32), ("recent", C.c_int32), ("to", C.POINTER(C.c_uint64)), ("weight", C.c_void_p), ("position", C.c_void_p),
+                ("token_off", C.POINTER(C.c_int64)), ("kept", C.c_void_p), ("weight_out", C.c_void_p), ("position_out", C.c_void_p),
+                ("out_off", C.POINTER(C.c_int64))]
 
 
 class AdmissionParamsC(C.Structure):
@@ -152,6 +168,10 @@ def load_library() -> C.CDLL:
         "relaygr_kv_pool_write": (C.c_int, [vp, i32, P(KvRowsC), vp, i64, vp, i64, vp]),
         "relaygr_kv_pool_read": (C.c_int, [vp, i32, P(KvRowsC), vp, i64, vp, i64, vp]),
         "relaygr_cache_attend": (C.c_int, [vp, vp, i32, P(KvRowsC), i32, vp, i64, vp, i64, vp]),
+        "relaygr_rope_init": (C.c_int, [P(RopeC), i32, i32, C.c_double, C.c_double, i32, C.c_double, C.c_double, C.c_float]),
+        "relaygr_rotary": (C.c_int, [P(ModelConfigC), P(RopeC), i32, vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
+        "relaygr_cache_attend_scored": (C.c_int, [vp, vp, i32, P(KvRowsC), i32, P(ScoringC), vp, i64, vp, i64, vp, vp, vp]),
+        "relaygr_kv_pool_evict": (C.c_int, [vp, P(KvRowsC), P(KvEvictionC), vp]),
         "relaygr_last_error": (C.c_char_p, []),
     }
     for name, (res, args) in sig.items():
@@ -399,10 +419,10 @@ def _kv_rows_array(what: str, pool: KvPool, rows: KvRows, t: torch.Tensor):
     """(address, elements between rows) of a tensor [rows, d_model] or [rows, heads, d_head] on the pool's device."""
     d, n, shape, stride = pool.cfg.d_model, rows.n_rows, t.shape, t.stride()
     if len(shape) == 2:
-        ok = shape[0] == n and shape[1] == d and stride[1] == 1
+        ok = shape[0] == n and shape[1] == d and (n == 0 or stride[1] == 1)     # (the strides of nothing mean nothing)
     else:
         heads = pool.cfg.n_heads
-        ok = len(shape) == 3 and tuple(shape) == (n, heads, d // heads) and stride[2] == 1 and (heads == 1 or stride[1] == d // heads)
+        ok = len(shape) == 3 and tuple(shape) == (n, heads, d // heads) and (n == 0 or (stride[2] == 1 and (heads == 1 or stride[1] == d // heads)))
     if not ok or t.dtype != _torch_dtype(pool.dtype) or t.device != pool.slab.device:
         raise RelayGRError(RELAYGR_EINVAL, f"{what}: needs {n} rows of {d} adjacent {pool.dtype} elements on {pool.slab.device}, got "
                                            f"{tuple(shape)} of {t.dtype} on {t.device} with strides {stride}")
@@ -469,6 +489,193 @@ def relaygr_cache_attend(ctx: Context, pool: KvPool, layer: int, rows: KvRows, q
     _check(load_library().relaygr_cache_attend(ctx.handle, pool.handle, layer, rows.ref, int(causal), qp, qs, op, os_,
                                                torch._C._cuda_getCurrentRawStream(pool.slab.device.index)))
     return out
+
+
+# ---- positions, scores, masks and eviction ------------------------------------------------------
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+
+
+class Rope:
+    """relaygr_rope: the frequencies of rotary positions.  layout: "half" or "interleaved" pairs; factor, original_len, low, high: how positions are
+    stretched (include/relaygr.h); gain: what turned features are multiplied with."""
+
+    def __init__(self, dim: int, base: float = 10000.0, layout: str = "half", factor: float = 1.0, original_len: int = 0, low: float = 1.0,
+                 high: float = 32.0, gain: float = 1.0):
+        if layout not in ROPE_LAYOUTS:
+            raise RelayGRError(RELAYGR_EINVAL, f"unknown layout {layout!r}")
+        self.c = RopeC()
+        _check(load_library().relaygr_rope_init(C.byref(self.c), dim, ROPE_LAYOUTS[layout], base, factor, original_len, low, high, gain))
+        self.ref = C.byref(self.c)
+
+
+def _device_guard(device: torch.device, stream):
+    """What a call on tensors of a device has to be made under to be the default one, of that device's current stream; None if it is that already."""
+    if stream is not None:
+        s = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
+        if s.device != device:
+            raise RelayGRError(RELAYGR_EINVAL, f"a stream of {s.device} for tensors on {device}")
+        return torch.cuda.stream(s)
+    return None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _vector(what: str, t: Optional[torch.Tensor], dtype, device, n: Optional[int] = None):
+    """Address of a vector on the device, of n elements if n is given; None for none."""
+    if t is None:
+        return None
+    if t.dim() != 1 or t.dtype != dtype or t.device != device or (t.numel() > 1 and t.stride(0) != 1) or (n is not None and t.numel() != n):
+        raise RelayGRError(RELAYGR_EINVAL, f"{what}: needs {'' if n is None else n} adjacent {dtype} elements on {device}, got {tuple(t.shape)} of {t.dtype} on "
+                                           f"{t.device} with strides {t.stride()}")
+    return t.data_ptr() if t.numel() else None
+
+
+def _rotary_rows(what: str, cfg: ModelConfigC, n: int, device, t: torch.Tensor):
+    """(address, elements between rows) of a tensor [rows, d_model] or [rows, heads, d_head]."""
+    d, heads, shape, stride = cfg.d_model, cfg.n_heads, tuple(t.shape), t.stride()
+    ok = shape == (n, d) and (n == 0 or stride[1] == 1) or shape == (n, heads, d // heads) and (n == 0 or (stride[2] == 1 and (heads == 1 or stride[1] == d // heads)))
+    if not ok or t.dtype != _DTYPES_BY_CODE[cfg.dtype] or t.device != device:
+        raise RelayGRError(RELAYGR_EINVAL, f"{what}: needs {n} rows of {d} adjacent {_DTYPES_BY_CODE[cfg.dtype]} elements on {device}, got {shape} of {t.dtype} on "
+                                           f"{t.device} with strides {stride}")
+    return (t.data_ptr() if n else None), (stride[0] if n > 1 else d)
+
+
+_DTYPES_BY_CODE = {RELAYGR_DTYPE_FP32: torch.float32, RELAYGR_DTYPE_BF16: torch.bfloat16, RELAYGR_DTYPE_FP16: torch.float16}
+
+
+def relaygr_rotary(cfg: ModelConfigC, rope: Rope, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None, transposed: bool = False,
+                   q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
+    """Rows of q (and of k) turned by their positions (int32 [rows]): q, or (q, k), made here if q_out and k_out are not given; q_out may be q, k_out k.
+    transposed: by the opposite angle, which is the gradient's."""
+    device = q.device
+    if device.type != "cuda":
+        raise RelayGRError(RELAYGR_EINVAL, f"rotary: q is on {device}")
+    if k is None and k_out is not None:
+        raise RelayGRError(RELAYGR_EINVAL, "rotary: k_out without k")
+    guard = _device_guard(device, stream)
+    if guard is not None:
+        with guard:
+            return relaygr_rotary(cfg, rope, positions, q, k, transposed, q_out, k_out)
+    n = q.shape[0]
+    pos = _vector("rotary: positions", positions, torch.int32, device, n)
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=device) if q_out is None else q_out
+    qp, qs = _rotary_rows("rotary: q", cfg, n, device, q)
+    qo, qos = _rotary_rows("rotary: q_out", cfg, n, device, q_out)
+    kp = ko = None
+    ks = kos = 0
+    if k is not None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=device) if k_out is None else k_out
+        kp, ks = _rotary_rows("rotary: k", cfg, n, device, k)
+        ko, kos = _rotary_rows("rotary: k_out", cfg, n, device, k_out)
+    _check(load_library().relaygr_rotary(C.byref(cfg), rope.ref, n, pos, int(transposed), qp, qs, qo, qos, kp, ks, ko, kos,
+                                         torch._C._cuda_getCurrentRawStream(device.index)))
+    return q_out if k is None else (q_out, k_out)
+
+
+def _host_vector(what: str, x, dtype, n: Optional[int] = None):
+    a = np.array(x, dtype=dtype)
+    if a.ndim != 1 or (n is not None and a.size != n):
+        raise RelayGRError(RELAYGR_EINVAL, f"{what}: has shape {a.shape}" + ("" if n is None else f", ({n},) is needed"))
+    return a
+
+
+class Scoring:
+    """relaygr_scoring: scores and masks of relaygr_cache_attend_scored (include/relaygr.h has the formulas).
+
+    Device tensors: slopes fp32 [heads]; row_first, row_end, row_position int32 [rows]; key_position int32, user u's token j at token_off[u] + j.
+    Host: cap, window, prefix [users], token_off [users].  Made once, used in any number of calls of batches of these sizes; the tensors' contents, prefix and token_off may
+    change between them in place."""
+
+    def __init__(self, cap: float = 0.0, slopes: Optional[torch.Tensor] = None, window: int = 0, prefix: Optional[Sequence[int]] = None,
+                 row_first: Optional[torch.Tensor] = None, row_end: Optional[torch.Tensor] = None, row_position: Optional[torch.Tensor] = None,
+                 key_position: Optional[torch.Tensor] = None, token_off: Optional[Sequence[int]] = None):
+        self.slopes, self.row_first, self.row_end, self.row_position, self.key_position = slopes, row_first, row_end, row_position, key_position
+        self.prefix = None if prefix is None else _host_vector("Scoring: prefix", prefix, np.int32)
+        self.token_off = None if token_off is None else _host_vector("Scoring: token_off", token_off, np.int64)
+        if key_position is not None and token_off is None:
+            raise RelayGRError(RELAYGR_EINVAL, "Scoring: key_position without token_off")
+        self.tensors = [("slopes", slopes, torch.float32), ("row_first", row_first, torch.int32), ("row_end", row_end, torch.int32),
+                        ("row_position", row_position, torch.int32), ("key_position", key_position, torch.int32)]
+        self.c = ScoringC(cap, window, None, None if self.prefix is None else self.prefix.ctypes.data_as(C.POINTER(C.c_int32)), None, None, None, None,
+                          None if self.token_off is None else self.token_off.ctypes.data_as(C.POINTER(C.c_int64)))
+        self.ref = C.byref(self.c)
+
+    def bind(self, pool: KvPool, rows: KvRows) -> None:
+        """Checks the arrays against a batch and puts the tensors' addresses into the struct."""
+        device = pool.slab.device
+        for name, t, dtype in self.tensors:
+            if t is None:
+                continue
+            n = pool.cfg.n_heads if name == "slopes" else None if name == "key_position" else rows.n_rows
+            setattr(self.c, name, _vector("Scoring: " + name, t, dtype, device, n))
+        for name in ("prefix", "token_off"):
+            a = getattr(self, name)
+            if a is not None and a.size != rows.n_users:
+                raise RelayGRError(RELAYGR_EINVAL, f"Scoring: {name} of {a.size} users for a batch of {rows.n_users}")
+
+
+def _tokens_fit(what: str, rows: KvRows, lens, token_off: np.ndarray, t: Optional[torch.Tensor]) -> None:
+    """Refuses a tensor that does not hold the tokens of every user."""
+    if t is not None and rows.n_users and int((token_off + lens).max()) > t.numel():
+        raise RelayGRError(RELAYGR_EINVAL, f"{what}: {t.numel()} elements do not hold every user's tokens")
+
+
+def _lens(pool: KvPool, rows: KvRows):
+    return rows.key_len if rows.key_len is not None else np.array([relaygr_kv_pool_entry_len(pool, int(h)) for h in rows.handles], dtype=np.int32)
+
+
+def relaygr_cache_attend_scored(ctx: Context, pool: KvPool, layer: int, rows: KvRows, q: torch.Tensor, scoring: Scoring, causal: bool = False,
+                                out: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None, weight_out: Optional[torch.Tensor] = None,
+                                stream=None) -> torch.Tensor:
+    """relaygr_cache_attend with scores and masks of `scoring`: [rows, d_model] (made here if not given).  weight_out (fp32, user u's token j at
+    scoring.token_off[u] + j): weight, or 0 without one, plus what each token received from these rows; weight alone is added to in place."""
+    if ctx.scratch.device != pool.slab.device:
+        raise RelayGRError(RELAYGR_EINVAL, f"cache_attend_scored: a context on {ctx.scratch.device} for a pool on {pool.slab.device}")
+    guard = _kv_guard(pool, stream)
+    if guard is not None:
+        with guard:
+            return relaygr_cache_attend_scored(ctx, pool, layer, rows, q, scoring, causal, out, weight, weight_out)
+    qp, qs = _kv_rows_array("cache_attend_scored: q", pool, rows, q)
+    scoring.bind(pool, rows)
+    weight_out = weight if weight_out is None else weight_out
+    wi = _vector("cache_attend_scored: weight", weight, torch.float32, pool.slab.device)
+    wo = _vector("cache_attend_scored: weight_out", weight_out, torch.float32, pool.slab.device)
+    if scoring.token_off is not None and (weight_out is not None or scoring.key_position is not None):
+        lens = _lens(pool, rows)
+        for name, t in (("key_position", scoring.key_position), ("weight", weight), ("weight_out", weight_out)):
+            _tokens_fit("cache_attend_scored: " + name, rows, lens, scoring.token_off, t)
+    out, op, os_ = _result_rows("cache_attend_scored: out", pool, rows, out)
+    _check(load_library().relaygr_cache_attend_scored(ctx.handle, pool.handle, layer, rows.ref, int(causal), scoring.ref, qp, qs, op, os_, wi, wo,
+                                                      torch._C._cuda_getCurrentRawStream(pool.slab.device.index)))
+    return out
+
+
+def relaygr_kv_pool_evict(pool: KvPool, rows: KvRows, weight: torch.Tensor, token_off: Sequence[int], first: int = 0, recent: int = 0,
+                          to: Optional[Sequence[int]] = None, kept: Optional[torch.Tensor] = None, weight_out: Optional[torch.Tensor] = None,
+                          position: Optional[torch.Tensor] = None, position_out: Optional[torch.Tensor] = None, out_off: Optional[Sequence[int]] = None,
+                          stream=None) -> torch.Tensor:
+    """Evicts the tokens with the least weight: rows.row_off says how many of the first rows.key_len tokens of each entry stay.  Returns `kept` (int32
+    [rows.n_rows], made here if not given): the places of those that stay."""
+    guard = _kv_guard(pool, stream)
+    if guard is not None:
+        with guard:
+            return relaygr_kv_pool_evict(pool, rows, weight, token_off, first, recent, to, kept, weight_out, position, position_out, out_off)
+    device, n = pool.slab.device, rows.n_users
+    token_off = _host_vector("kv_pool_evict: token_off", token_off, np.int64, n)
+    out_off = None if out_off is None else _host_vector("kv_pool_evict: out_off", out_off, np.int64, n)
+    to = None if to is None else _host_vector("kv_pool_evict: to", to, np.uint64, n)
+    kept = torch.empty(rows.n_rows, dtype=torch.int32, device=device) if kept is None else kept
+    e = KvEvictionC(first, recent, None if to is None else to.ctypes.data_as(C.POINTER(C.c_uint64)), _vector("kv_pool_evict: weight", weight, torch.float32, device),
+                    _vector("kv_pool_evict: position", position, torch.int32, device), token_off.ctypes.data_as(C.POINTER(C.c_int64)),
+                    _vector("kv_pool_evict: kept", kept, torch.int32, device, rows.n_rows), _vector("kv_pool_evict: weight_out", weight_out, torch.float32, device),
+                    _vector("kv_pool_evict: position_out", position_out, torch.int32, device),
+                    None if out_off is None else out_off.ctypes.data_as(C.POINTER(C.c_int64)))
+    lens = _lens(pool, rows)
+    for name, t in (("weight", weight), ("position", position)):
+        _tokens_fit("kv_pool_evict: " + name, rows, lens, token_off, t)
+    counts = np.diff(rows.row_off)
+    for name, t in (("weight_out", weight_out), ("position_out", position_out)):
+        _tokens_fit("kv_pool_evict: " + name, rows, counts, rows.row_off[:-1] if out_off is None else out_off, t)
+    _check(load_library().relaygr_kv_pool_evict(pool.handle, rows.ref, C.byref(e), torch._C._cuda_getCurrentRawStream(device.index)))
+    return kept
 
 
 # ---- DRAM tier -------------------------------------------------------------------------------

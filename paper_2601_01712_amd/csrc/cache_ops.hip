@@ -8,6 +8,7 @@
 
 #include "attend8.h"
 #include "attend_rules.h"
+#include "cache_rows.h"
 #include "errors.h"
 #include "kv8.h"
 
@@ -20,45 +21,6 @@ using namespace relaygr;
   } while (0)
 
 namespace {
-
-// Rows of a [rows, d] array must be 16-byte aligned runs of d elements.
-int check_rows_array(const char* what, const char* name, const void* base, int64_t stride, int d) {
-  if (!base) return fail(RELAYGR_EINVAL, "%s: %s is null", what, name);
-  if (((uintptr_t)base & 15) || stride % 8) return fail(RELAYGR_EINVAL, "%s: rows of %s are not 16-byte aligned", what, name);
-  if (stride < d) return fail(RELAYGR_EINVAL, "%s: %s has a row stride of %lld elements, below d_model", what, name, (long long)stride);
-  return RELAYGR_OK;
-}
-
-// The batch's entries, after the checks that all three calls share.
-int resolve_rows(const char* what, KvPool* pool, int32_t layer, const relaygr_kv_rows* r, std::vector<PoolEntry>* entries) {
-  if (!pool || !r) return fail(RELAYGR_EINVAL, "%s: null argument", what);
-  if (!pool->q8) return fail(RELAYGR_EINVAL, "%s: the pool does not hold 8-bit K/V", what);
-  if (layer < 0 || layer >= pool->cfg.n_layers) return fail(RELAYGR_EINVAL, "%s: layer %d out of range", what, layer);
-  if (r->n_users < 0) return fail(RELAYGR_EINVAL, "%s: n_users < 0", what);
-  if (r->row_off && r->row_off[0] != 0) return fail(RELAYGR_EINVAL, "%s: row offsets must start at 0", what);
-  if (r->n_users == 0) return RELAYGR_OK;
-  if (!r->handles || !r->row_off) return fail(RELAYGR_EINVAL, "%s: null handles or row offsets", what);
-  for (int u = 0; u < r->n_users; ++u)
-    if (r->row_off[u + 1] < r->row_off[u]) return fail(RELAYGR_EINVAL, "%s: row offsets not monotone at user %d", what, u);
-  entries->resize(r->n_users);
-  const int found = pool->resolve_all(r->handles, r->n_users, entries->data());
-  if (found < r->n_users) return fail(RELAYGR_ENOENT, "%s: user %d: stale or unknown handle", what, found);
-  return RELAYGR_OK;
-}
-
-// launch(storage type, d_head)
-template <class F>
-void by_head(const relaygr_model_config& cfg, F launch) {
-  auto by_dh = [&](auto h) {
-    switch (cfg.d_model / cfg.n_heads) {
-      case 32: launch(h, std::integral_constant<int, 32>()); break;
-      case 64: launch(h, std::integral_constant<int, 64>()); break;
-      default: launch(h, std::integral_constant<int, 128>()); break;
-    }
-  };
-  if (cfg.dtype == RELAYGR_DTYPE_FP16) by_dh(F16());
-  else by_dh(Bf16());
-}
 
 // once: rows and codes are more than the caches hold.
 template <bool WRITE, int USERS>

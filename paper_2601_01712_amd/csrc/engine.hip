@@ -25,6 +25,7 @@
 #include "kv8.h"
 #include "kv_pool.h"
 #include "rowwise.h"
+#include "scored_ops.h"
 #include "staging.h"
 
 using namespace relaygr;
@@ -1114,24 +1115,44 @@ static int run(relaygr_ctx* c, relaygr_kv_pool* pool, const relaygr_batch* b, Mo
   return rc;
 }
 
-extern "C" int relaygr_cache_attend(relaygr_ctx* c, relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, int32_t causal, const void* q,
-                                    int64_t q_stride, void* out, int64_t out_stride, void* hip_stream) {
-  if (!c || !pool) return fail(RELAYGR_EINVAL, "cache_attend: null argument");
-  KvPool* kp = reinterpret_cast<KvPool*>(pool);
+// One attention call over a pool in the context's scratch and stream order: enqueue(call) plans and launches it.
+template <class F>
+static int attend_in_context(const char* what, relaygr_ctx* c, KvPool* kp, AttendCall call, void* hip_stream, F enqueue) {
   const relaygr_model_config &a = kp->cfg, &m = c->cfg;
   if (a.n_layers != m.n_layers || a.d_model != m.d_model || a.n_heads != m.n_heads || a.dtype != m.dtype)
-    return fail(RELAYGR_EINVAL, "cache_attend: pool and context were created for different model shapes");
+    return fail(RELAYGR_EINVAL, "%s: pool and context were created for different model shapes", what);
   std::lock_guard<std::mutex> call_lock(c->mu);
   hipStream_t st = (hipStream_t)hip_stream;
   const size_t wp = wpack_bytes(c->cfg);
   const bool capturing = stream_is_capturing(st);      // (as in run)
-  const AttendCall call = {rows, layer, causal, q, q_stride, out, out_stride, c->attn_form == RELAYGR_ATTN_SOFTMAX, c->n_cus, c->scratch + wp, c->scratch_bytes - wp,
-                           capturing ? nullptr : (uint32_t*)(c->scratch + wp - kArrivalBytes)};
+  call.softmax = c->attn_form == RELAYGR_ATTN_SOFTMAX;
+  call.n_cus = c->n_cus;
+  call.scratch = c->scratch + wp;
+  call.scratch_bytes = c->scratch_bytes - wp;
+  call.arrived = capturing ? nullptr : (uint32_t*)(c->scratch + wp - kArrivalBytes);
   if (!capturing && c->has_call && c->last_stream != st) HIP_TRY(order_behind(st, c->last_stream, c->call_done));
   int rc;
-  try { rc = attend8(kp, call, st); } catch (...) { rc = fail(RELAYGR_EINVAL, "cache_attend: out of host memory"); }
+  try { rc = enqueue(call, st); } catch (...) { rc = fail(RELAYGR_EINVAL, "%s: out of host memory", what); }
   if (!capturing) { c->last_stream = st; c->has_call = true; }
   return rc;
+}
+
+extern "C" int relaygr_cache_attend(relaygr_ctx* c, relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, int32_t causal, const void* q,
+                                    int64_t q_stride, void* out, int64_t out_stride, void* hip_stream) {
+  if (!c || !pool) return fail(RELAYGR_EINVAL, "cache_attend: null argument");
+  KvPool* kp = reinterpret_cast<KvPool*>(pool);
+  const AttendCall call = {rows, layer, causal, q, q_stride, out, out_stride, false, 0, nullptr, 0, nullptr};
+  return attend_in_context("cache_attend", c, kp, call, hip_stream, [&](const AttendCall& x, hipStream_t st) { return attend8(kp, x, st); });
+}
+
+extern "C" int relaygr_cache_attend_scored(relaygr_ctx* c, relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, int32_t causal,
+                                           const relaygr_scoring* scoring, const void* q, int64_t q_stride, void* out, int64_t out_stride,
+                                           const float* weight_in, float* weight_out, void* hip_stream) {
+  if (!c || !pool) return fail(RELAYGR_EINVAL, "cache_attend_scored: null argument");
+  KvPool* kp = reinterpret_cast<KvPool*>(pool);
+  const AttendCall call = {rows, layer, causal, q, q_stride, out, out_stride, false, 0, nullptr, 0, nullptr};
+  return attend_in_context("cache_attend_scored", c, kp, call, hip_stream,
+                           [&](const AttendCall& x, hipStream_t st) { return scored8(kp, ScoredCall{x, scoring, weight_in, weight_out}, st); });
 }
 
 extern "C" int relaygr_prefill_prefix(relaygr_ctx* ctx, relaygr_kv_pool* pool, const relaygr_batch* batch, void* hip_stream) {

@@ -1,0 +1,104 @@
+// C-ABI entry points of rotary positions (rotary.h).
+#include "rotary.h"
+
+#include <math.h>
+
+#include <algorithm>
+
+#include "../../include/relaygr.h"
+#include "cache_rows.h"
+#include "errors.h"
+
+using namespace relaygr;
+
+extern "C" int relaygr_rope_init(relaygr_rope* out, int32_t dim, int32_t layout, double base, double factor, int32_t original_len, double low, double high,
+                                 float gain) {
+  static const char* what = "rope_init";
+  if (!out) return fail(RELAYGR_EINVAL, "%s: null argument", what);
+  if (dim < 2 || dim > 2 * kRotaryPairs || dim % 2) return fail(RELAYGR_EINVAL, "%s: %d features are not pairs of a head", what, dim);
+  if (layout != RELAYGR_ROPE_HALF && layout != RELAYGR_ROPE_INTERLEAVED) return fail(RELAYGR_EINVAL, "%s: unknown layout %d", what, layout);
+  if (!(base > 0) || !isfinite(base) || !(factor > 0) || !isfinite(factor) || !isfinite(gain)) return fail(RELAYGR_EINVAL, "%s: base, factor or gain", what);
+  if (original_len < 0 || (original_len > 0 && (!isfinite(low) || !isfinite(high) || !(low < high)))) return fail(RELAYGR_EINVAL, "%s: original length, low or high", what);
+  *out = relaygr_rope();
+  out->dim = dim; out->layout = layout; out->gain = gain;
+  const long double turn = 6.283185307179586476925286766559L;
+  for (int i = 0; i < dim / 2; ++i) {
+    const long double f = powl((long double)base, -2.0L * i / dim);
+    long double keep = 0;
+    if (original_len > 0) {
+      keep = (original_len * f / turn - low) / ((long double)high - low);
+      keep = keep < 0 ? 0 : keep > 1 ? 1 : keep;
+    }
+    const long double turns = f * (keep + (1 - keep) / factor) / turn;
+    if (!isfinite(turns)) return fail(RELAYGR_EINVAL, "%s: a frequency beyond any", what);
+    const long double scaled = roundl(ldexpl(turns - floorl(turns), 64));
+    out->turns[i] = scaled >= 0x1p64L ? 0 : (uint64_t)scaled;
+  }
+  return RELAYGR_OK;
+}
+
+namespace {
+
+// Lanes take all heads of a row while that leaves the chip enough of them: the angles are a lane's first work, some 25 instructions each, and the loads of its heads are
+// what hides the memory.
+template <class T>
+void launch_rotary(RotaryParams p, hipStream_t st) {
+  constexpr int E = RotaryType<T>::E;
+  const RotaryUnit unit = p.units_sh == 0 ? kRotaryInterleaved : (p.dim / 2) % E ? kRotaryOdd : kRotaryHalf;      // (units_sh carries the layout here)
+  const int units = unit == kRotaryHalf ? p.dim / 2 / E + (p.dh - p.dim) / E : p.dh / E;
+  p.units_sh = 0;
+  while (1 << p.units_sh < units) ++p.units_sh;
+  const int64_t lanes = (int64_t)p.n_rows << p.units_sh;
+  p.heads_per = p.n_heads;
+  while (p.heads_per > 1 && lanes * (p.n_heads / p.heads_per) < 2048 * 64) p.heads_per = (p.heads_per + 1) / 2;
+  const int32_t rows = p.n_rows;
+  for (int32_t row = 0; row < rows; row += p.n_rows) {
+    p.n_rows = (int32_t)std::min<int64_t>(rows - row, (1ll << 31) >> p.units_sh);      // (a launch counts its threads in 32 bits)
+    const dim3 grid((unsigned)((((int64_t)p.n_rows << p.units_sh) + 255) / 256), (unsigned)((p.n_heads + p.heads_per - 1) / p.heads_per));
+    switch (unit) {
+      case kRotaryHalf: hipLaunchKernelGGL((rotary_kernel<T, kRotaryHalf>), grid, dim3(256), 0, st, p); break;
+      case kRotaryInterleaved: hipLaunchKernelGGL((rotary_kernel<T, kRotaryInterleaved>), grid, dim3(256), 0, st, p); break;
+      default: hipLaunchKernelGGL((rotary_kernel<T, kRotaryOdd>), grid, dim3(256), 0, st, p); break;
+    }
+    p.position += p.n_rows;
+    for (RotaryArray& x : p.x) { x.in += x.in ? p.n_rows * x.in_stride : 0; x.out += x.in ? p.n_rows * x.out_stride : 0; }
+  }
+}
+
+}  // namespace
+
+extern "C" int relaygr_rotary(const relaygr_model_config* cfg, const relaygr_rope* rope, int32_t n_rows, const int32_t* positions, int32_t transposed,
+                              const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, void* k_out,
+                              int64_t k_out_stride, void* hip_stream) {
+  static const char* what = "rotary";
+  if (!cfg || !rope) return fail(RELAYGR_EINVAL, "%s: null argument", what);
+  if (relaygr_kv_footprint_bytes(cfg, 1) == 0) return fail(RELAYGR_EINVAL, "%s: unsupported model configuration", what);
+  const int d = cfg->d_model, dh = d / cfg->n_heads, e = elem_bytes(*cfg);
+  if (rope->dim < 2 || rope->dim % 2 || rope->dim > dh) return fail(RELAYGR_EINVAL, "%s: %d features of a head of %d", what, rope->dim, dh);
+  if (rope->layout != RELAYGR_ROPE_HALF && rope->layout != RELAYGR_ROPE_INTERLEAVED) return fail(RELAYGR_EINVAL, "%s: unknown layout %d", what, rope->layout);
+  if (n_rows < 0) return fail(RELAYGR_EINVAL, "%s: n_rows < 0", what);
+  if (n_rows == 0) return RELAYGR_OK;
+  if (!positions || ((uintptr_t)positions & 3)) return fail(RELAYGR_EINVAL, "%s: positions are null or not aligned", what);
+  if (!k != !k_out) return fail(RELAYGR_EINVAL, "%s: k without k_out, or k_out without k", what);
+  int rc;
+  if ((rc = check_rows_array(what, "q", q, q_stride, d, e)) != RELAYGR_OK || (rc = check_rows_array(what, "q_out", q_out, q_out_stride, d, e)) != RELAYGR_OK) return rc;
+  if (k && ((rc = check_rows_array(what, "k", k, k_stride, d, e)) != RELAYGR_OK || (rc = check_rows_array(what, "k_out", k_out, k_out_stride, d, e)) != RELAYGR_OK)) return rc;
+  if ((q == q_out && q_stride != q_out_stride) || (k && k == k_out && k_stride != k_out_stride))
+    return fail(RELAYGR_EINVAL, "%s: rows in place must stay where they are", what);
+  RotaryParams p = {};
+  p.x[0] = {(const char*)q, (char*)q_out, q_stride * e, q_out_stride * e};
+  p.x[1] = {(const char*)k, (char*)k_out, k_stride * e, k_out_stride * e};
+  p.position = positions;
+  p.n_rows = n_rows; p.n_heads = cfg->n_heads; p.dh = dh; p.dim = rope->dim;
+  p.units_sh = rope->layout == RELAYGR_ROPE_INTERLEAVED ? 0 : 1;
+  p.transposed = transposed ? 1 : 0; p.gain = rope->gain;
+  for (int i = 0; i < kRotaryPairs; ++i) p.turns[i] = rope->turns[i];
+  (void)hipGetLastError();
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (cfg->dtype == RELAYGR_DTYPE_FP32) launch_rotary<float>(p, st);
+  else if (cfg->dtype == RELAYGR_DTYPE_FP16) launch_rotary<F16>(p, st);
+  else launch_rotary<Bf16>(p, st);
+  hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return fail(RELAYGR_EHIP, "launch %s: %s", what, hipGetErrorString(err));
+  return RELAYGR_OK;
+}

@@ -1,0 +1,192 @@
+"""Rotary positions against the formula in extended precision."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_01712_amd as rg
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TORCH = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+HALF_STEP = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8, "fp16": 2.0 ** -11}
+HALF_LEAST = {"fp32": 2.0 ** -150, "bf16": 2.0 ** -134, "fp16": 2.0 ** -25}     # half of the least subnormal
+
+
+def frequencies(dim, base=10000.0, factor=1.0, original_len=0, low=1.0, high=32.0):
+    i = np.arange(dim // 2, dtype=np.longdouble)
+    f = np.longdouble(base) ** (-2 * i / dim)
+    r = np.clip((original_len * f / (2 * np.pi) - low) / (np.longdouble(high) - low), 0, 1) if original_len else np.zeros_like(f)
+    return f * (r + (1 - r) / factor)
+
+
+def rotate(x, pos, dim, layout, freq, gain=1.0, transposed=False):
+    """(result, what a kernel may be off by before it rounds): x [rows, heads, dh] in 64 bits."""
+    t = pos.astype(np.longdouble)[:, None] * freq[None]
+    t = np.remainder(t, 2 * np.longdouble("3.14159265358979323846264338327950288")).astype(np.float64)[:, None] * (-1.0 if transposed else 1.0)
+    a, b = (np.arange(dim // 2), np.arange(dim // 2, dim)) if layout == "half" else (np.arange(0, dim, 2), np.arange(1, dim, 2))
+    y, off = x.copy(), np.zeros_like(x)
+    y[..., a] = gain * (x[..., a] * np.cos(t) - x[..., b] * np.sin(t))
+    y[..., b] = gain * (x[..., a] * np.sin(t) + x[..., b] * np.cos(t))
+    # sine and cosine to 2^-23 (their angle to 2^-25 of pi/4, the series, its sums), times the gain, a product and a sum; the angle itself: the frequency's 64 bits and the 80-bit
+    # reference at 2^31 positions
+    size = gain * (np.abs(x[..., a]) + np.abs(x[..., b]))
+    off[..., a] = off[..., b] = size * (2.0 ** -22 + np.abs(pos.astype(np.float64))[:, None, None] * 2.0 ** -60)
+    return y, off
+
+
+def check(got, want, off, dtype, dim):
+    got = got.double().cpu().numpy().reshape(want.shape)
+    bound = off + HALF_STEP[dtype] * (np.abs(want) + off) + HALF_LEAST[dtype]
+    worst = (np.abs(got - want) / bound)[..., :dim]
+    assert np.isfinite(got).all() and worst.max(initial=0.0) <= 1.0, worst.max()
+
+
+def rows(rng, n, d, dtype):
+    t = torch.from_numpy(rng.standard_normal((n, d)).astype(np.float32) * 2).to(TORCH[dtype])
+    return t, t.double().numpy()
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("d,heads", [(128, 4), (512, 8), (256, 2), (1024, 8), (128, 1)])
+def test_whole_parts_and_odd_parts_of_heads(d, heads, dtype, layout, transposed):
+    dh = d // heads
+    cfg = rg.make_config(2, d, heads, dtype)
+    rng = np.random.default_rng(d + heads)
+    for dim in sorted({2, 6, dh // 2, dh // 2 + 2, dh - 2, dh}):
+        for n in (1, 5, 67):
+            (q, q64), (k, k64) = rows(rng, n, d, dtype), rows(rng, n, d, dtype)
+            pos = rng.integers(0, 5000, n).astype(np.int32)
+            got = rg.relaygr_rotary(cfg, rg.Rope(dim, layout=layout), torch.from_numpy(pos).to(DEV), q.to(DEV), k.to(DEV), transposed=transposed)
+            for g, x, raw in zip(got, (q64, k64), (q, k)):
+                want, off = rotate(x.reshape(n, heads, dh), pos, dim, layout, frequencies(dim), transposed=transposed)
+                check(g, want, off, dtype, dim)
+                assert torch.equal(g.cpu().view(n, heads, dh)[..., dim:], raw.view(n, heads, dh)[..., dim:]), "features behind the turned ones"
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_far_and_negative_positions_scaled_frequencies_and_gain(dtype):
+    d, heads, dh = 256, 4, 64
+    cfg = rg.make_config(1, d, heads, dtype)
+    rng = np.random.default_rng(5)
+    pos = np.array([0, 1, -1, 2 ** 24 + 1, 2 ** 31 - 1, -2 ** 31, 123456789, 4096, -77], np.int32)
+    q, q64 = rows(rng, len(pos), d, dtype)
+    for kw in (dict(), dict(base=500000.0), dict(factor=8.0), dict(factor=4.0, original_len=4096), dict(factor=40.0, original_len=2048, low=0.5, high=3.5), dict(base=0.5)):
+        for gain in (1.0, 1.139):
+            got = rg.relaygr_rotary(cfg, rg.Rope(dh, gain=gain, **kw), torch.from_numpy(pos).to(DEV), q.to(DEV))
+            check(got, *rotate(q64.reshape(-1, heads, dh), pos, dh, "half", frequencies(dh, **kw), gain=float(np.float32(gain))), dtype, dh)
+
+
+@pytest.mark.parametrize("layout,dim", [("half", 64), ("half", 20), ("half", 48), ("interleaved", 64), ("interleaved", 22)])
+@pytest.mark.parametrize("dtype", ["fp32", "fp16"])
+def test_in_place_strides_and_neighbours(dtype, layout, dim):
+    """Rows that are columns of a wider array, turned where they stand, many and few of them: the same bits as into another array, the columns beside them as they were."""
+    d, heads = 512, 8
+    cfg = rg.make_config(1, d, heads, dtype)
+    rope = rg.Rope(dim, layout=layout)
+    for n in (1, 3, 40, 9000):
+        gen = torch.Generator(device=DEV)
+        gen.manual_seed(n)
+        wide = torch.randn((n, 2048), generator=gen, device=DEV).to(TORCH[dtype])
+        before = wide.clone()
+        pos = torch.randint(0, 1 << 20, (n,), generator=gen, device=DEV, dtype=torch.int32)
+        want = rg.relaygr_rotary(cfg, rope, pos, wide[:, 512:1024].contiguous(), wide[:, 1536:].contiguous())
+        q, k = wide[:, 512:1024], wide[:, 1536:].view(n, heads, -1)
+        got = rg.relaygr_rotary(cfg, rope, pos, q, k, q_out=q, k_out=k)
+        assert got[0] is q and torch.equal(wide[:, 512:1024], want[0]) and torch.equal(wide[:, 1536:], want[1])
+        assert torch.equal(wide[:, :512], before[:, :512]) and torch.equal(wide[:, 1024:1536], before[:, 1024:1536])
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_the_gradient_is_the_rotation_back(layout):
+    """<R x, y> = <x, R' y> for every x and y, and differences of <R x, y> in each element are R' y: R is linear, so that a step of any size gives them."""
+    d, heads, n = 128, 2, 3
+    cfg = rg.make_config(1, d, heads, "fp32")
+    rope = rg.Rope(48, layout=layout, gain=1.25)
+    rng = np.random.default_rng(9)
+    x, y = (torch.from_numpy(rng.standard_normal((n, d)).astype(np.float32)).to(DEV) for _ in range(2))
+    pos = torch.tensor([3, 1000, 77777], dtype=torch.int32, device=DEV)
+    grad = rg.relaygr_rotary(cfg, rope, pos, y, transposed=True).double()
+    base = (rg.relaygr_rotary(cfg, rope, pos, x).double() * y.double()).sum()
+    # 2^-21 of every product: sine, cosine, gain and the sums on both sides
+    tol = 2.0 ** -21 * 4 * 1.25
+    assert abs(float(base - (x.double() * grad).sum())) <= tol * float((x.abs().double() * 2).sum() * y.abs().max())
+    for row, f in ((0, 0), (0, 23), (1, 24), (1, 47), (2, 48), (2, 64), (2, 127), (0, 100)):
+        step = torch.zeros_like(x)
+        step[row, f] = 1.0
+        slope = (rg.relaygr_rotary(cfg, rope, pos, step).double() * y.double()).sum()
+        assert abs(float(slope - grad[row, f])) <= tol * float(y.abs().max()) * 2
+
+
+def test_there_and_back_and_relative_scores():
+    """Turned and turned back; and products of turned rows depend on the distance of their positions alone."""
+    d, heads, dh = 256, 4, 64
+    cfg = rg.make_config(1, d, heads, "fp32")
+    rope = rg.Rope(dh)
+    rng = np.random.default_rng(11)
+    q, k = (torch.from_numpy(rng.standard_normal((1, d)).astype(np.float32)).to(DEV).expand(50, d).contiguous() for _ in range(2))
+    pos = torch.arange(0, 50 * 40000001, 40000001, dtype=torch.int64).to(torch.int32).to(DEV)
+    near, far = rg.relaygr_rotary(cfg, rope, pos, q), rg.relaygr_rotary(cfg, rope, pos + 37, k)
+    s = (near.double() * far.double()).view(50, heads, dh).sum(-1)
+    size = (q.double().abs().sum(-1) * k.double().abs().max()).max()
+    assert float((s - s[:1]).abs().max()) <= 2.0 ** -20 * float(size)
+    back = rg.relaygr_rotary(cfg, rope, pos, near, transposed=True)
+    assert float((back - q).abs().max()) <= 2.0 ** -20 * 2 * float(q.abs().max())
+
+
+def test_nan_stays_with_its_pair():
+    d, heads = 128, 2
+    cfg = rg.make_config(1, d, heads, "bf16")
+    q = torch.ones((2, d), dtype=torch.bfloat16, device=DEV)
+    q[0, 70] = float("nan")
+    q[1, 60] = float("inf")
+    pos = torch.tensor([5, 9], dtype=torch.int32, device=DEV)
+    got = rg.relaygr_rotary(cfg, rg.Rope(32), pos, q)
+    bad = torch.zeros((2, d), dtype=torch.bool, device=DEV)
+    bad[0, 70] = bad[0, 86] = True
+    assert torch.equal(torch.isnan(got), bad) and float(got[1, 60]) == float("inf")
+
+
+def test_captured_calls_streams_and_nothing_to_do():
+    d, heads = 256, 4
+    cfg, rope = rg.make_config(1, d, heads, "bf16"), rg.Rope(64)
+    rng = np.random.default_rng(13)
+    q = rows(rng, 30, d, "bf16")[0].to(DEV)
+    pos = torch.arange(30, dtype=torch.int32, device=DEV)
+    out = torch.empty_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        rg.relaygr_rotary(cfg, rope, pos, q, q_out=out)
+    for _ in range(3):
+        q.copy_(rows(rng, 30, d, "bf16")[0])
+        pos += 11
+        want = rg.relaygr_rotary(cfg, rope, pos, q)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        for s in (side, side.cuda_stream):
+            got = rg.relaygr_rotary(cfg, rope, pos, q, stream=s)
+            torch.cuda.synchronize()
+            assert torch.equal(got, want)
+    assert rg.relaygr_rotary(cfg, rope, pos[:0], q[:0]).shape == (0, d)
+    a, b = rg.relaygr_rotary(cfg, rope, pos[:0], q[:0].view(0, 4, 64), q[:0])
+    assert a.shape == (0, 4, 64) and b.shape == (0, d)
+
+
+def test_refusals():
+    d, heads = 256, 4
+    cfg, rope = rg.make_config(1, d, heads, "bf16"), rg.Rope(64)
+    q = torch.zeros((4, d), dtype=torch.bfloat16, device=DEV)
+    pos = torch.zeros(4, dtype=torch.int32, device=DEV)
+    wide = torch.zeros((4, d + 4), dtype=torch.bfloat16, device=DEV)
+    for kw in (dict(rope=rg.Rope(66)), dict(positions=pos[:3]), dict(positions=pos.long()), dict(positions=pos.cpu()), dict(q=q.half()), dict(q=q.float()), dict(q=q.cpu()), dict(k=q[:3]),
+               dict(q=wide[:, 4:]), dict(q_out=q[:2]), dict(k_out=q), dict(q=torch.zeros((4, 4, 128), dtype=torch.bfloat16, device=DEV)),
+               dict(q=wide[:, :d], q_out=q.clone(), k=wide[:, :d])):
+        args = dict(rope=rope, positions=pos, q=q, k=None) | kw
+        with pytest.raises(rg.RelayGRError) as e:
+            rg.relaygr_rotary(cfg, args.pop("rope"), args.pop("positions"), args.pop("q"), args.pop("k"), **args)
+        assert e.value.code == rg.RELAYGR_EINVAL

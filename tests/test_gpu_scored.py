@@ -1,0 +1,371 @@
+"""Scored attention over an 8-bit pool, and the tokens' weights, against the formula in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_01712_amd as rg
+from q8_util import TORCH, attend_rule, context_for, held, model, offsets, pool_for, values
+from scored_util import scored, visible
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def dev(a, dtype=np.int32):
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a, dtype=dtype)).to(DEV)
+
+
+class Case:
+    """Entries of the given lengths in layer 1 of 2, their cached values in 64 bits, a context, and room for the tokens' weights with gaps between users."""
+
+    def __init__(self, d, heads, dtype, form, lens, rows, seed=0, room=0, check=None):
+        self.d, self.heads, self.dh, self.dtype, self.form, self.lens, self.rows = d, heads, d // heads, dtype, form, lens, rows
+        self.rng = np.random.default_rng(seed)
+        self.ctx = context_for(model(d, heads, dtype, form), len(lens), max(1, sum(rows), room))
+        self.pool, self.handles = pool_for(self.ctx.cfg, dtype, lens)
+        (k, k64), (v, v64) = (values(self.rng, sum(lens), d, dtype) for _ in range(2))
+        rg.relaygr_kv_pool_write(self.pool, 1, rg.KvRows(self.handles, offsets(lens)), k.to(DEV), v.to(DEV))
+        at = offsets(lens)
+        self.checked = list(range(len(lens))) if check is None else check
+        self.k, self.v = ([None if u not in self.checked else held(x[at[u]:at[u + 1]].reshape(n, heads, d // heads), dtype) for u, n in enumerate(lens)] for x in (k64, v64))
+        self.q, self.q64 = values(self.rng, sum(rows), d, dtype)
+        self.q = self.q.to(DEV)
+        self.row_off = offsets(rows)
+        self.token_off = np.cumsum([3] + [n + 5 for n in lens])[:-1]
+        self.n_tokens = int(self.token_off[-1] + lens[-1] + 7)
+        self.slopes = (2.0 ** -np.linspace(1, 8, heads)).astype(np.float32)
+
+    def call(self, causal=False, key_len=None, cap=0.0, bias=False, prefix=None, first=None, end=None, window=0, row_pos=None, key_pos=None, weigh=False, weight=None, **kw):
+        lens = self.lens if key_len is None else key_len
+        tokens = None
+        if key_pos is not None:
+            tokens = np.full(self.n_tokens, -2 ** 30, np.int32)
+            for o, p in zip(self.token_off, key_pos):
+                tokens[o:o + len(p)] = p
+        scoring = rg.Scoring(cap=cap, slopes=dev(self.slopes, np.float32) if bias else None, window=window, prefix=prefix, row_first=dev(first), row_end=dev(end), row_position=dev(row_pos),
+                             key_position=dev(tokens), token_off=self.token_off)
+        weights = torch.full((self.n_tokens,), -7.0, device=DEV) if weigh and weight is None else None
+        out = rg.relaygr_cache_attend_scored(self.ctx, self.pool, 1, rg.KvRows(self.handles, self.row_off, key_len=key_len), self.q, scoring, causal=causal, weight=weight,
+                                             weight_out=weights, **kw)
+        self.args = dict(causal=causal, lens=lens, cap=cap, bias=bias, prefix=prefix, first=first, end=end, window=window, row_pos=row_pos, key_pos=key_pos)
+        return (out, weights if weight is None else weight) if weigh else out
+
+    def want(self, u):
+        a = self.args
+        n, m = a["lens"][u], self.rows[u]
+        r = slice(self.row_off[u], self.row_off[u + 1])
+        see = visible(n, m, a["causal"], a["prefix"][u] if a["prefix"] is not None else 0, None if a["first"] is None else a["first"][r], None if a["end"] is None else a["end"][r], a["window"])
+        row_pos = a["row_pos"][r] if a["row_pos"] is not None else (n - m + np.arange(m) if a["causal"] else np.full(m, n))
+        key_pos = a["key_pos"][u] if a["key_pos"] is not None else np.arange(n)
+        q = self.q64[r].reshape(m, self.heads, self.dh)
+        return scored(q, self.k[u][:n], self.v[u][:n], see, self.form, self.dtype, a["cap"], self.slopes if a["bias"] else None, row_pos, key_pos[:n]), see
+
+    def check(self, out, weights=None, before=0.0):
+        got = out.double().cpu().numpy()
+        if weights is not None:
+            w = weights.double().cpu().numpy()
+            untouched = np.ones(self.n_tokens, bool)
+            for o, n in zip(self.token_off, self.args["lens"]):
+                untouched[o:o + n] = False
+            assert (w[untouched] == -7.0).all(), "beside the users' tokens"
+        for u in self.checked:
+            (want, bound, total, dtotal), see = self.want(u)
+            g = got[self.row_off[u]:self.row_off[u + 1]].reshape(want.shape)
+            assert np.isfinite(g).all(), u
+            assert (g[~see.any(axis=1)] == 0).all(), "rows that see nothing"
+            off = np.abs(g - want) / bound
+            assert off.max(initial=0.0) <= 1.0, f"user {u} ({self.rows[u]} rows, {self.lens[u]} keys): {off.max():.2f} of the bound at {np.unravel_index(off.argmax(), off.shape)}"
+            if weights is not None:
+                n = self.args["lens"][u]
+                x = w[self.token_off[u]:self.token_off[u] + n]
+                off = np.abs(x - total - before) / (dtotal + 2.0 ** -23 * np.abs(before) + 2.0 ** -100)
+                assert off.max(initial=0.0) <= 1.0, f"user {u}: weights {off.max():.2f} of the bound at {off.argmax()}"
+                assert (x[~see.any(axis=0)] == before).all(), "tokens that nobody sees"
+
+
+LENS, ROWS = [1, 64, 65, 200, 63, 700, 129, 2], [1, 3, 33, 64, 65, 31, 0, 130]
+
+
+def sessions(case, mean=40):
+    """First tokens of the rows' sessions, some beyond what the row sees, some negative."""
+    return case.rng.integers(-20, 2 * mean, case.row_off[-1]) + np.concatenate([np.maximum(np.arange(m) + n - m - mean, -5) for n, m in zip(case.lens, case.rows)])
+
+
+@pytest.mark.parametrize("form", ["silu", "softmax"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d,heads", [(128, 4), (256, 4), (256, 8), (512, 8), (512, 4), (1024, 8), (128, 1)])
+def test_everything_at_once(d, heads, dtype, form):
+    c = Case(d, heads, dtype, form, LENS, ROWS, seed=d + heads)
+    prefix = [0, 70, 3, 64, 5, 65, 9, 1]
+    for causal in (False, True):
+        key_pos = [np.cumsum(c.rng.integers(1, 4, n)) for n in LENS]
+        row_pos = np.concatenate([k[-1] + 1 + np.arange(m) for k, m in zip(key_pos, ROWS)])
+        c.check(*c.call(causal=causal, cap=4.0, bias=True, prefix=prefix, first=sessions(c), row_pos=row_pos, key_pos=key_pos, weigh=True))
+        c.check(*c.call(causal=causal, cap=30.0, bias=True, window=50, weigh=True))
+
+
+@pytest.mark.parametrize("form", ["silu", "softmax"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("kind", ["plain", "cap", "cap_small", "cap_large", "cap_huge", "bias", "positions", "row_positions", "prefix", "first", "end", "first_end", "window", "window_prefix", "window_1"])
+def test_one_thing_at_a_time(kind, causal, form):
+    c = Case(256, 4, "bf16", form, [300, 64, 1, 130, 500], [40, 70, 2, 1, 33], seed=len(kind))
+    n_rows = int(c.row_off[-1])
+    end = c.rng.integers(-3, 320, n_rows)
+    key_pos = [np.cumsum(c.rng.integers(1, 1000, n)) for n in c.lens]
+    row_pos = c.rng.integers(-1000, 500000, n_rows)
+    kw = {"plain": {}, "cap": dict(cap=2.0), "cap_small": dict(cap=0.125), "cap_large": dict(cap=200.0), "cap_huge": dict(cap=1e6), "bias": dict(bias=True),
+          "positions": dict(bias=True, key_pos=key_pos, row_pos=row_pos), "row_positions": dict(bias=True, row_pos=row_pos), "prefix": dict(prefix=[100, 0, 7, 200, 65]),
+          "first": dict(first=sessions(c)), "end": dict(end=end), "first_end": dict(first=end - c.rng.integers(-2, 60, n_rows), end=end), "window": dict(window=100),
+          "window_prefix": dict(window=70, prefix=[64, 1, 0, 63, 130]), "window_1": dict(window=1)}[kind]
+    c.check(*c.call(causal=causal, weigh=True, **kw))
+    if kind == "plain":
+        same = rg.relaygr_cache_attend(c.ctx, c.pool, 1, rg.KvRows(c.handles, c.row_off), c.q, causal=causal)
+        c.check(same)
+
+
+@pytest.mark.parametrize("form", ["silu", "softmax"])
+@pytest.mark.parametrize("lens,rows", [([16000], [1]), ([9000, 5], [2, 1]), ([5000, 300, 7000], [40, 1, 3]), ([4000], [300]), ([12000] * 3, [5, 9, 33]), ([3000] * 20, [4] * 20),
+                                       ([2500] * 70, [1] * 70)])
+def test_long_histories_cut_along_the_keys(lens, rows, form):
+    c = Case(512 if len(lens) < 20 else 128, 8 if len(lens) < 20 else 4, "bf16", form, lens, rows, seed=sum(rows), check=[0, len(lens) - 1])
+    c.check(*c.call(cap=20.0, bias=True, weigh=True))
+    c.check(*c.call(causal=True, window=1500, prefix=[100] * len(lens), weigh=True))
+    # rows that see a few tokens of a long history: pieces with nothing in them
+    first = np.concatenate([np.full(m, max(n - 100, 0)) for n, m in zip(lens, rows)])
+    c.check(*c.call(first=first, end=first + 50, weigh=True))
+    c.check(*c.call(end=np.zeros(sum(rows)), weigh=True))
+
+
+@pytest.mark.parametrize("form", ["silu", "softmax"])
+def test_launches_that_do_not_keep_the_codes(form):
+    """Few rows over more than the caches hold."""
+    lens, rows = [8200] * 66, [1] * 65 + [2]
+    assert attend_rule(rows, lens, 8, 64)["once"] == 1
+    c = Case(512, 8, "bf16", form, lens, rows, seed=3, room=8192, check=[0, 65])
+    c.check(*c.call(bias=True, cap=25.0, weigh=True))
+
+
+@pytest.mark.parametrize("form", ["silu", "softmax"])
+@pytest.mark.parametrize("rows", [1, 7, 8, 9, 31, 100])
+def test_weights_from_kept_scores_and_from_keys_again(rows, form):
+    """Up to eight rows leave their scores in scratch if it has the room: either way the same weights, added to what was there, in place too, the same bits in every call."""
+    c = Case(256, 4, "fp16", form, [1000, 77, 400], [rows, rows, 0], seed=rows, room=4096)
+    out, w = c.call(cap=10.0, causal=True, weigh=True)
+    c.check(out, w)
+    again = c.call(cap=10.0, causal=True, weigh=True)
+    assert torch.equal(again[0], out) and torch.equal(again[1], w)
+    start = torch.full_like(w, 0.5)
+    start[w == -7.0] = -7.0
+    _, more = c.call(cap=10.0, causal=True, weigh=True, weight=start.clone())
+    c.check(out, more, before=0.5)
+    small = context_for(model(256, 4, "fp16", form), 1, 2 * rows)
+    c.ctx = small
+    c.check(*c.call(cap=10.0, causal=True, weigh=True))
+
+
+def test_idle_users_pass_their_weights_on():
+    c = Case(128, 2, "bf16", "softmax", [100, 40, 70], [0, 0, 0], seed=1)
+    before = torch.rand(c.n_tokens, device=DEV)
+    after = torch.full_like(before, -7.0)
+    scoring = rg.Scoring(token_off=c.token_off)
+    rows = rg.KvRows(c.handles, c.row_off)
+    rg.relaygr_cache_attend_scored(c.ctx, c.pool, 1, rows, c.q, scoring, weight=before, weight_out=after)
+    mine = np.zeros(c.n_tokens, bool)
+    for o, n in zip(c.token_off, c.lens):
+        mine[o:o + n] = True
+    mine = torch.from_numpy(mine).to(DEV)
+    assert torch.equal(after[mine], before[mine]) and bool((after[~mine] == -7.0).all())
+
+
+def test_large_scores_infinities_and_caps():
+    """Scores beyond exp's range, with a cap that brings them back; rows of infinities and NaN are those rows' own."""
+    c = Case(128, 4, "bf16", "softmax", [200, 90], [33, 5], seed=5)
+    c.q = (c.q.float() * 500).to(torch.bfloat16)
+    c.q64 = c.q.double().cpu().numpy()
+    c.check(*c.call(weigh=True))
+    c.check(*c.call(weigh=True, cap=50.0))
+    c.check(*c.call(weigh=True, cap=1000.0, bias=True))
+    clean = c.call(cap=50.0)
+    c.q[3], c.q[7] = float("nan"), float("inf")
+    got = c.call(cap=50.0)
+    keep = torch.ones(38, dtype=torch.bool, device=DEV)
+    keep[3] = keep[7] = False
+    assert torch.equal(got[keep], clean[keep]) and bool(torch.isnan(got[3]).all())
+
+
+@pytest.mark.parametrize("form", ["silu", "softmax"])
+@pytest.mark.parametrize("d,heads,dtype", [(256, 4, "bf16"), (128, 4, "fp16"), (256, 2, "fp16")])
+def test_nan_reaches_the_rows_that_see_it_only(d, heads, dtype, form):
+    """NaN in K or V of one token of one head: rows that do not see the token, by a window, a session or their own place, stay as they are, and so do the other tokens' weights of
+    rows that do not see it."""
+    n, m, at, dh = 250, 100, 170, d // heads
+    for what in "kv":
+        c = Case(d, heads, dtype, form, [n], [m], seed=41)
+        first = c.rng.integers(100, 240, m)
+        calls = [dict(causal=True), dict(causal=True, window=15), dict(first=first), dict(end=first), dict(causal=True, prefix=[171], window=3), dict(causal=True, prefix=[170], window=3)]
+        clean = [c.call(**kw) for kw in calls]
+        k, v = (torch.from_numpy(x[0]).to(TORCH[dtype]).to(DEV).view(n, d) for x in (c.k, c.v))
+        (k if what == "k" else v)[at, dh + 5] = float("nan")
+        rg.relaygr_kv_pool_write(c.pool, 1, rg.KvRows(c.handles, [0, n]), k, v)
+        for kw, before in zip(calls, clean):
+            got = c.call(**kw)
+            sees = torch.from_numpy(visible(n, m, kw.get("causal", False), kw.get("prefix", [0])[0], kw.get("first"), kw.get("end"), kw.get("window", 0))[:, at])
+            bad = torch.isnan(got).view(m, heads, dh).cpu()
+            cols = torch.zeros(heads, dh, dtype=torch.bool)
+            if what == "k":
+                cols[1] = True
+            else:
+                cols[1, 5] = True
+            assert torch.equal(bad, sees[:, None, None] & cols[None]), kw
+            assert torch.equal(got.view(m, heads, dh)[:, 2:], before.view(m, heads, dh)[:, 2:])
+        _, w = c.call(first=np.full(m, at + 1), weigh=True)
+        mine = w[c.token_off[0]:c.token_off[0] + n]
+        assert bool(torch.isfinite(mine).all()) and bool((mine[:at + 1] == 0).all())
+
+
+def test_key_lengths_and_columns_of_wider_arrays():
+    c = Case(256, 4, "bf16", "silu", [300, 200, 64], [20, 7, 3], seed=7)
+    c.check(*c.call(key_len=[0, 130, 64], cap=8.0, bias=True, weigh=True))
+    wide = torch.full((30, 768), 3.0, dtype=torch.bfloat16, device=DEV)
+    wide[:, 256:512] = c.q
+    want = c.call(window=40, bias=True)
+    rows = rg.KvRows(c.handles, c.row_off)
+    scoring = rg.Scoring(window=40, slopes=dev(c.slopes, np.float32))
+    out = wide[:, 512:].view(30, 4, 64)
+    rg.relaygr_cache_attend_scored(c.ctx, c.pool, 1, rows, wide[:, 256:512], scoring, out=out)
+    assert torch.equal(wide[:, 512:], want) and bool((wide[:, :256] == 3.0).all()) and torch.equal(wide[:, 256:512], c.q)
+
+
+def test_captured_calls_replay_on_new_rows():
+    """Two graphs of one context, with its eager calls between their replays; weights add up over replays."""
+    c = Case(512, 8, "bf16", "softmax", [3000, 400], [20, 3], seed=47, room=4096)
+    rows = rg.KvRows(c.handles, c.row_off)
+    first = dev(np.concatenate([np.full(20, 100), np.full(3, 30)]))
+    scoring = rg.Scoring(cap=20.0, slopes=dev(c.slopes, np.float32), row_first=first, token_off=c.token_off)
+    one = rg.KvRows(c.handles[:1], [0, 1])
+    alone = rg.Scoring(window=500, token_off=c.token_off[:1])
+    outs, weights = (torch.empty_like(c.q), torch.empty_like(c.q[:1])), [torch.zeros(c.n_tokens, device=DEV) for _ in range(2)]
+
+    def step(i, out, w):
+        if i == 0:
+            return rg.relaygr_cache_attend_scored(c.ctx, c.pool, 1, rows, c.q, scoring, out=out, weight=w)
+        return rg.relaygr_cache_attend_scored(c.ctx, c.pool, 1, one, c.q[:1], alone, out=out, weight=w)
+    graphs = []
+    for i in range(2):
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            step(i, outs[i], weights[i])
+    eager = [torch.zeros(c.n_tokens, device=DEV) for _ in range(2)]
+    for turn in range(4):
+        c.q.copy_(values(c.rng, 23, c.d, c.dtype)[0])
+        first += 7
+        for i in ((0, 1), (1, 0))[turn % 2]:
+            graphs[i].replay()
+            want = step(i, None, eager[i])
+            torch.cuda.synchronize()
+            # (a captured call joins its pieces by a launch of its own, in the same order)
+            assert torch.equal(outs[i], want) and torch.equal(weights[i], eager[i])
+
+
+def test_two_streams_share_a_context():
+    c = Case(256, 4, "bf16", "softmax", [9000, 7000], [2, 30], seed=53)
+    out, w = c.call(cap=9.0, weigh=True)
+    c.check(out, w)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = [c.call(cap=9.0, weigh=True, stream=s) for _ in range(5) for s in (a, b)]
+    torch.cuda.synchronize()
+    for o, x in got:
+        assert torch.equal(o, out)
+        for u, n in zip(c.token_off, c.lens):
+            assert torch.equal(x[u:u + n], w[u:u + n])
+
+
+def test_little_scratch():
+    """No room for pieces or kept scores: the same answers; none for the rows' sums: refused, nothing written."""
+    d, heads = 128, 1
+    for form in ("silu", "softmax"):
+        c = Case(d, heads, "bf16", form, [16384], [300], seed=83)
+        c.check(*c.call(cap=5.0, weigh=True))
+        c.ctx = context_for(model(d, heads, "bf16", form), 1, 1)
+        c.check(*c.call(cap=5.0, weigh=True))
+        c.check(*c.call(causal=True, weigh=True))
+    c = Case(d, 4, "bf16", "softmax", [64], [200000], seed=84, check=[])
+    c.ctx = context_for(model(d, 4, "bf16", "softmax"), 1, 1)
+    assert rg.relaygr_scratch_bytes(c.ctx.cfg, 1, 0, 1) - 2 * 5 * d * d * 2 < 200000 * 4 * 4
+    out = torch.full_like(c.q, 3.0)
+    with pytest.raises(rg.RelayGRError) as e:
+        c.call(weigh=True, out=out)
+    assert e.value.code == rg.RELAYGR_ENOSPC
+    torch.cuda.synchronize()
+    assert bool((out == 3.0).all())
+    c.call()
+
+
+def test_weights_and_positions_beyond_4_gib():
+    """Tokens' arrays with a user's tokens behind 2^32 bytes of others."""
+    c = Case(128, 2, "bf16", "softmax", [200], [9], seed=67)
+    far = (1 << 30) + 12345
+    w = torch.full((far + 300,), -7.0, device=DEV)
+    pos = torch.full((far + 300,), 1 << 20, dtype=torch.int32, device=DEV)
+    pos[far:far + 200] = torch.arange(200, device=DEV, dtype=torch.int32)
+    want, near = c.call(bias=True, weigh=True)
+    scoring = rg.Scoring(slopes=dev(c.slopes, np.float32), key_position=pos, token_off=[far])
+    out = rg.relaygr_cache_attend_scored(c.ctx, c.pool, 1, rg.KvRows(c.handles, c.row_off), c.q, scoring, weight_out=w)
+    assert torch.equal(out, want) and torch.equal(w[far:far + 200], near[3:203])
+    assert bool((w[far - 1000:far] == -7.0).all()) and bool((w[far + 200:] == -7.0).all())
+
+
+def test_entries_beyond_4_gib_of_the_slab():
+    d, heads, dtype = 1024, 8, "bf16"
+    ctx = context_for(model(d, heads, dtype, "softmax", layers=16), 1, 70)
+    tile = rg.relaygr_kv_pool_bytes_for_q8(ctx.cfg, 64, 64)
+    before = (1 << 32) // tile + 3
+    pool = rg.KvPool(ctx.cfg, dtype, (before + 4) * tile, 64, quantized=True)
+    rg.relaygr_kv_pool_alloc(pool, 1, before * 64)
+    h = rg.relaygr_kv_pool_alloc(pool, 2, 200)
+    rng = np.random.default_rng(67)
+    (k, k64), (v, v64), (q, q64) = (values(rng, n, d, dtype) for n in (200, 200, 70))
+    rg.relaygr_kv_pool_write(pool, 15, rg.KvRows([h], [0, 200]), k.to(DEV), v.to(DEV))
+    w = torch.empty(200, device=DEV)
+    out = rg.relaygr_cache_attend_scored(ctx, pool, 15, rg.KvRows([h], [0, 70]), q.to(DEV), rg.Scoring(cap=6.0, token_off=[0]), causal=True, weight_out=w)
+    kh, vh = held(k64.reshape(200, heads, -1), dtype), held(v64.reshape(200, heads, -1), dtype)
+    want, bound, total, dtotal = scored(q64.reshape(70, heads, -1), kh, vh, visible(200, 70, True), "softmax", dtype, cap=6.0)
+    assert (np.abs(out.double().cpu().numpy().reshape(want.shape) - want) <= bound).all()
+    assert (np.abs(w.double().cpu().numpy() - total) <= dtotal).all()
+
+
+def test_refusals():
+    c = Case(256, 4, "bf16", "softmax", [100, 50], [2, 3], seed=59)
+    good = dict(cap=1.0, slopes=dev(c.slopes, np.float32), token_off=c.token_off)
+
+    def code(scoring=None, weight=None, rows=None, pool=None, ctx=None, layer=1, **kw):
+        out = torch.full((5, 256), 3.0, dtype=torch.bfloat16, device=DEV)
+        w = torch.full((c.n_tokens,), 3.0, device=DEV) if weight is None else weight
+        rows = rg.KvRows(c.handles, c.row_off) if rows is None else rows
+        with pytest.raises(rg.RelayGRError) as e:
+            rg.relaygr_cache_attend_scored(ctx or c.ctx, pool or c.pool, layer, rows, c.q, rg.Scoring(**(good if scoring is None else good | scoring)), out=out, weight_out=w, **kw)
+        torch.cuda.synchronize()
+        assert bool((out == 3.0).all()) and bool((w == 3.0).all())
+        return e.value.code
+    i32 = dict(dtype=torch.int32, device=DEV)
+    for s in (dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")), dict(window=-1), dict(prefix=[0, -1]), dict(prefix=[0]), dict(token_off=[0]), dict(token_off=[-1, 200]),
+              dict(token_off=[0, 99]), dict(token_off=[49, 0]), dict(token_off=[0, c.n_tokens - 49]), dict(slopes=torch.zeros(3, device=DEV)), dict(slopes=torch.zeros(4)),
+              dict(slopes=torch.zeros(4, dtype=torch.float64, device=DEV)), dict(row_first=torch.zeros(4, **i32)), dict(row_end=torch.zeros(5, dtype=torch.int64, device=DEV)),
+              dict(row_position=torch.zeros(10, **i32)[::2]), dict(key_position=torch.zeros(c.n_tokens - 20, **i32)), dict(row_end=torch.zeros(5, dtype=torch.int32))):
+        assert code(scoring=s) == rg.RELAYGR_EINVAL, s
+    assert code(weight=torch.full((c.n_tokens,), 3.0, dtype=torch.float16, device=DEV)) == rg.RELAYGR_EINVAL
+    assert code(scoring=dict(token_off=None)) == rg.RELAYGR_EINVAL
+    assert code(layer=2) == rg.RELAYGR_EINVAL and code(rows=rg.KvRows([c.handles[0], 12345], [0, 2, 5], key_len=[100, 50])) == rg.RELAYGR_ENOENT
+    assert code(rows=rg.KvRows(c.handles, [0, 2, 5], key_len=[101, 50])) == rg.RELAYGR_EINVAL
+    assert code(ctx=context_for(model(512, 8, "bf16"), 1, 8)) == rg.RELAYGR_EINVAL
+    p16 = rg.KvPool(c.ctx.cfg, "bf16", 4 * rg.relaygr_kv_pool_bytes_for(c.ctx.cfg, 64, 64), 64)
+    h16 = rg.relaygr_kv_pool_alloc(p16, 1, 100)
+    assert code(pool=p16, rows=rg.KvRows([h16], [0, 5]), scoring=dict(token_off=[0])) == rg.RELAYGR_EINVAL
+    with pytest.raises(rg.RelayGRError):
+        rg.Scoring(key_position=torch.zeros(5, **i32))
+    # nothing to do is no error
+    assert rg.relaygr_cache_attend_scored(c.ctx, c.pool, 0, rg.KvRows([], [0]), c.q[:0], rg.Scoring()).shape == (0, 256)
+    assert rg.relaygr_cache_attend_scored(c.ctx, c.pool, 0, rg.KvRows(c.handles, [0, 0, 0]), c.q[:0], rg.Scoring()).shape == (0, 256)

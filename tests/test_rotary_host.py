@@ -1,0 +1,81 @@
+"""Rotary positions without a GPU: frequencies as they are kept, and every refusal that is made before anything is enqueued."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_01712_amd as rg
+from paper_2601_01712_amd import binding as B
+
+
+def test_frequencies_are_fractions_of_a_turn():
+    tau = 2 * np.longdouble("3.14159265358979323846264338327950288")
+    for dim, base in ((2, 10000.0), (64, 10000.0), (128, 500000.0), (6, 0.25), (20, 1.0)):
+        rope = rg.Rope(dim, base)
+        for i in range(dim // 2):
+            f = np.longdouble(base) ** (np.longdouble(-2 * i) / dim) / tau
+            want = float((f - np.floor(f)))
+            got = rope.c.turns[i] / 2.0 ** 64
+            assert abs(got - want) <= 2.0 ** -50 * max(want, 2.0 ** -10), (dim, base, i)
+        assert all(rope.c.turns[i] == 0 for i in range(dim // 2, 64))
+
+
+def test_stretched_frequencies():
+    plain, all_of_them = rg.Rope(64), rg.Rope(64, factor=8.0)
+    for i in range(32):
+        assert abs(all_of_them.c.turns[i] * 8 - plain.c.turns[i]) <= 16
+    some = rg.Rope(64, factor=8.0, original_len=4096, low=1.0, high=32.0)
+    kept = stretched = between = 0
+    for i in range(32):
+        n = 4096 * 10000.0 ** (-2 * i / 64) / (2 * math.pi)
+        r = some.c.turns[i] / plain.c.turns[i]
+        if n >= 32:
+            kept += 1
+            assert r == 1.0
+        elif n <= 1:
+            stretched += 1
+            assert abs(r - 0.125) < 1e-9
+        else:
+            between += 1
+            keep = (n - 1) / 31
+            assert abs(r - (keep + (1 - keep) / 8)) < 1e-9
+    assert kept and stretched and between
+
+
+def test_refused_frequencies():
+    lib, out = rg.load_library(), B.RopeC()
+
+    def init(dim=64, layout=0, base=10000.0, factor=1.0, original=0, low=1.0, high=32.0, gain=1.0, to=out):
+        return lib.relaygr_rope_init(C.byref(to) if to is not None else None, dim, layout, base, factor, original, low, high, gain)
+    assert init() == 0
+    nan, inf = float("nan"), float("inf")
+    for kw in (dict(dim=0), dict(dim=63), dict(dim=-2), dict(dim=130), dict(layout=2), dict(layout=-1), dict(base=0.0), dict(base=-1.0), dict(base=nan), dict(base=inf), dict(factor=0.0),
+               dict(factor=nan), dict(factor=inf), dict(gain=nan), dict(gain=inf), dict(original=-1), dict(original=10, low=2.0, high=2.0), dict(original=10, low=nan),
+               dict(original=10, high=inf), dict(to=None)):
+        assert init(**kw) == rg.RELAYGR_EINVAL and rg.relaygr_last_error(), kw
+    with pytest.raises(rg.RelayGRError):
+        rg.Rope(64, layout="other")
+
+
+def test_refused_calls():
+    lib, cfg, rope = rg.load_library(), rg.make_config(2, 256, 4, "bf16"), rg.Rope(64)
+
+    def call(cfg=cfg, rope=rope.c, n=3, pos=0x1000, q=0x10000, qs=256, qo=0x20000, qos=256, k=0x30000, ks=256, ko=0x40000, kos=256):
+        return lib.relaygr_rotary(C.byref(cfg) if cfg else None, C.byref(rope) if rope else None, n, pos, 0, q, qs, qo, qos, k, ks, ko, kos, None)
+    bad_dim, bad_layout = B.RopeC(), B.RopeC()
+    bad_dim.dim, bad_layout.dim, bad_layout.layout = 66, 64, 5
+    for kw in (dict(cfg=None), dict(rope=None), dict(rope=bad_dim), dict(rope=bad_layout), dict(n=-1), dict(pos=None), dict(pos=0x1002), dict(q=None), dict(qo=None), dict(ko=None), dict(k=None),
+               dict(q=0x10008), dict(qo=0x20002), dict(qs=255), dict(qs=248), dict(qos=260), dict(ks=0), dict(kos=-256), dict(qo=0x10000, qos=512),
+               dict(ko=0x30000, kos=264), dict(cfg=rg.make_config(2, 96, 3, "bf16")), dict(cfg=rg.make_config(2, 64, 2, "bf16"))):
+        assert call(**kw) == rg.RELAYGR_EINVAL and rg.relaygr_last_error(), kw
+    assert call(n=0, pos=None, q=None, qo=None, k=None, ko=None) == 0
+    # fp32: rows are 16-byte aligned at strides of 4
+    f32 = rg.make_config(1, 64, 2, "fp32")
+    assert call(cfg=f32, rope=rg.Rope(32).c, qs=66) == rg.RELAYGR_EINVAL
+
+
+def test_binding_refuses_tensors_on_the_host():
+    with pytest.raises(rg.RelayGRError):
+        rg.relaygr_rotary(rg.make_config(1, 128, 2, "bf16"), rg.Rope(64), torch.zeros(1, dtype=torch.int32), torch.zeros(1, 128, dtype=torch.bfloat16))
