@@ -43,21 +43,20 @@ int check_scoring(const relaygr_kv_rows* r, const relaygr_scoring& s, const floa
   return RELAYGR_OK;
 }
 
-template <typename H, int DH, bool SM, int USERS>
-void launch_scored(const ScoredParams<USERS>& p, int blocks, bool once, hipStream_t st) {
+// item_rows: of the launch's items, 16 or 32.
+template <typename H, int DH, bool SM, bool BIAS, int USERS>
+void launch_scored(const ScoredParams<USERS>& p, int item_rows, bool once, hipStream_t st) {
   const dim3 grid((unsigned)attend_groups(p.n_items, p.n_heads)), block(kAttendWaves * 64);
+  if (item_rows == 32) { hipLaunchKernelGGL((scored8_kernel<H, DH, SM, BIAS, USERS>), grid, block, 0, st, p); return; }
   if constexpr (USERS > kFewScoredUsers) {
-    if (once) { hipLaunchKernelGGL((scored8_kernel<H, DH, 1, SM, true, USERS>), grid, block, 0, st, p); return; }
+    if (once) { hipLaunchKernelGGL((scored8_few_kernel<H, DH, SM, BIAS, true, USERS>), grid, block, 0, st, p); return; }
   }
-  hipLaunchKernelGGL((scored8_kernel<H, DH, 1, SM, false, USERS>), grid, block, 0, st, p);
+  hipLaunchKernelGGL((scored8_few_kernel<H, DH, SM, BIAS, false, USERS>), grid, block, 0, st, p);
 }
 
-struct Work { int user, rows, keys, parts, prefix, tiles; int64_t saved0; };
+struct Work { int user, rows, keys, parts, prefix, tiles; };
 
 }  // namespace
-
-// Rows of a user up to which the scores are kept for the tokens' weights.
-static constexpr int kSavedRows = 8;
 
 int relaygr::scored8(KvPool* pool, const ScoredCall& call, hipStream_t st) {
   const AttendCall& c = call.attend;
@@ -78,10 +77,11 @@ int relaygr::scored8(KvPool* pool, const ScoredCall& call, hipStream_t st) {
     const int keys = r->key_len ? r->key_len[u] : entries[u].prefix_len, n = r->row_off[u + 1] - r->row_off[u];
     if (keys < 0 || keys > entries[u].prefix_len) return fail(RELAYGR_EINVAL, "%s: user %d: %d keys of an entry of %d tokens", what, u, keys, entries[u].prefix_len);
     const int prefix = s.prefix ? std::min(s.prefix[u], keys) : 0;
-    if (n == 0) { idle.push_back({u, 0, keys, 1, prefix, 0, 0}); continue; }
+    if (prefix >= 1 << 25) return fail(RELAYGR_EINVAL, "%s: user %d: a prefix of %d tokens is more than a launch takes", what, u, prefix);
+    if (n == 0) { idle.push_back({u, 0, keys, 1, prefix, 0}); continue; }
     // what an item's rows see at most: a window and the 32 or 64 tokens that its rows are apart
     const int64_t most = s.window > 0 ? std::min<int64_t>(keys, (int64_t)prefix + s.window + kTile) : keys;
-    work.push_back({u, n, keys, 1, prefix, (int)((most + kTile - 1) / kTile), 0});
+    work.push_back({u, n, keys, 1, prefix, (int)((most + kTile - 1) / kTile)});
     lens.push_back({n, (int)most});
     most_rows = std::max(most_rows, n);
   }
@@ -111,8 +111,7 @@ int relaygr::scored8(KvPool* pool, const ScoredCall& call, hipStream_t st) {
     lse = (float*)take(need);
   }
   AttendRule rule = attend_rule(lens, H, dh, c.n_cus);
-  rule.blocks = 1;
-  const int item_rows = 32 * rule.blocks;
+  const int item_rows = most_rows <= 16 ? 16 : 32;
   const size_t row_bytes = (size_t)d * 4 + (c.softmax ? (size_t)H * 16 : 0);
   const auto items_of = [&](const Work& w) { return ((int64_t)w.rows + item_rows - 1) / item_rows * w.parts; };
   int64_t partial_rows = 0, most_items = 0;
@@ -132,10 +131,11 @@ int relaygr::scored8(KvPool* pool, const ScoredCall& call, hipStream_t st) {
   float* part = partial_rows ? (float*)take((size_t)partial_rows * d * 4) : nullptr;
   float4* ml = partial_rows && c.softmax ? (float4*)take((size_t)partial_rows * H * 16) : nullptr;
   float* saved = nullptr;
+  int64_t saved_stride = 0;
   if (weigh && most_rows <= kSavedRows && !work.empty()) {
-    int64_t scores = 0;
-    for (Work& w : work) { w.saved0 = scores; scores += (int64_t)H * w.rows * ((w.keys + kTile - 1) / kTile * kTile); }
-    if ((size_t)scores * 4 <= left) saved = (float*)scratch;
+    for (const Work& w : work) saved_stride = std::max<int64_t>(saved_stride, ((int64_t)w.keys + kTile - 1) / kTile * kTile);
+    // (a row's place in it is a 32-bit offset from its user's first)
+    if (saved_stride * H * kSavedRows * 4 < 1ll << 31 && (size_t)r->row_off[r->n_users] * H * saved_stride * 4 <= left) saved = (float*)scratch;
   }
   std::stable_sort(work.begin(), work.end(), [](const Work& a, const Work& b) { return (int64_t)a.tiles * b.parts > (int64_t)b.tiles * a.parts; });    // the longest pieces first
 
@@ -144,26 +144,38 @@ int relaygr::scored8(KvPool* pool, const ScoredCall& call, hipStream_t st) {
   sc.slopes = s.slopes; sc.row_position = s.row_position; sc.key_position = s.key_position; sc.row_first = s.row_first; sc.row_end = s.row_end;
   sc.causal = c.causal ? 1 : 0; sc.window = s.window;
   const double alpha = 1.0 / std::sqrt((double)dh), log2e = 1.4426950408889634;
-  sc.score_mul = (float)(alpha * log2e);
-  if (s.cap > 0) { sc.cap = (float)(s.cap * log2e); sc.cap_mul = (float)(2.0 * alpha * log2e / s.cap); sc.cap_series = s.cap > kCapSeries; }
+  sc.mul = (float)(alpha * log2e);
+  if (s.cap > 0) {
+    sc.mul = (float)(-2.0 * s.cap * log2e); sc.add = (float)(s.cap * log2e); sc.cap_mul = (float)(2.0 * alpha * log2e / s.cap);
+    sc.cap_series = s.cap > kCapSeries;
+  }
   const char* slab = (const char*)pool->slab + c.layer * pool->layer_stride;
   const int64_t scales_off = q8_scales_off(cfg, c.layer) - c.layer * pool->layer_stride;
   const auto user_of_work = [&](const Work& w, int32_t item0, int32_t part0) -> ScoredUser {
-    return {(int32_t)entries[w.user].page0, r->row_off[w.user], w.rows, w.keys, item0, part0, w.parts, w.prefix, s.token_off ? s.token_off[w.user] : 0, w.saved0};
+    ScoredUser x = {};
+    x.page0 = (int32_t)entries[w.user].page0; x.row0 = r->row_off[w.user]; x.rows = w.rows; x.keys = w.keys; x.item0 = item0; x.part0 = part0;
+    x.cut = (uint32_t)w.parts | (uint32_t)w.prefix << 7; x.token0 = s.token_off ? s.token_off[w.user] : 0;
+    return x;
   };
 
+  const auto by_form = [&](auto go) {      // go(softmax form, bias)
+    if (c.softmax) { if (s.slopes) go(std::true_type(), std::true_type()); else go(std::true_type(), std::false_type()); }
+    else if (s.slopes) go(std::false_type(), std::true_type());
+    else go(std::false_type(), std::false_type());
+  };
   int32_t part0 = 0;
   auto launch = [&](auto users) -> int {
     constexpr int USERS = decltype(users)::value;
     ScoredParams<USERS> p = {};
     p.q = (const uint16_t*)c.q; p.out = (uint16_t*)c.out; p.q_stride = c.q_stride; p.out_stride = c.out_stride;
     p.slab = slab; p.page_bytes = (int64_t)pool->page_bytes; p.tile_stride = pool->tile_stride; p.scales_off = scales_off;
-    p.part = part; p.ml = ml; p.lse = lse; p.saved = saved;
+    p.part = part; p.ml = ml; p.lse = lse; p.saved = saved; p.saved_stride = saved_stride;
     p.d = d; p.n_heads = H; p.s = sc;
     ScoredParams<USERS> j = p;
+    const int launches = ((int)work.size() + USERS - 1) / USERS, per = ((int)work.size() + launches - 1) / launches;      // (as many users in each)
     for (size_t i = 0; i < work.size();) {
       p.n_users = 0; p.n_items = 0; j.n_users = 0; j.n_items = 0;
-      for (; i < work.size() && p.n_users < USERS; ++i) {
+      for (; i < work.size() && p.n_users < per; ++i) {
         const Work& w = work[i];
         if (!attend_fits(p.n_items + items_of(w), H)) break;      // (never a launch's first)
         p.users[p.n_users++] = user_of_work(w, p.n_items, part0);
@@ -177,8 +189,9 @@ int relaygr::scored8(KvPool* pool, const ScoredCall& call, hipStream_t st) {
       by_head(cfg, [&](auto h, auto dim) {
         using HT = decltype(h);
         constexpr int DH = decltype(dim)::value;
-        if (c.softmax) launch_scored<HT, DH, true>(p, rule.blocks, rule.once, st);
-        else launch_scored<HT, DH, false>(p, rule.blocks, rule.once, st);
+        by_form([&](auto sm, auto bias) {
+          if constexpr (USERS != kTokenUsers || decltype(bias)::value) launch_scored<HT, DH, decltype(sm)::value, decltype(bias)::value>(p, item_rows, rule.once, st);
+        });
         if (j.n_users == 0 || p.arrived) return;
         const dim3 grid((unsigned)(((int64_t)j.n_items * std::max(1, d / 256) + 3) / 4));
         if (c.softmax) hipLaunchKernelGGL((scored8_join_kernel<HT, DH, true, USERS>), grid, dim3(256), 0, st, j);
@@ -189,21 +202,23 @@ int relaygr::scored8(KvPool* pool, const ScoredCall& call, hipStream_t st) {
     return RELAYGR_OK;
   };
   if (!work.empty()) {
-    rc = (int)work.size() <= kFewScoredUsers && !rule.once ? launch(std::integral_constant<int, kFewScoredUsers>()) : launch(std::integral_constant<int, kScoredUsers>());
+    const bool few = (int)work.size() <= kFewScoredUsers && !(rule.once && item_rows == 16);
+    rc = few ? launch(std::integral_constant<int, kFewScoredUsers>())
+             : s.slopes && s.key_position ? launch(std::integral_constant<int, kTokenUsers>()) : launch(std::integral_constant<int, kScoredUsers>());
     if (rc != RELAYGR_OK) return rc;
   }
   if (!weigh) return RELAYGR_OK;
 
-  WeighParams<kScoredUsers> w = {};
+  WeighParams<kTokenUsers> w = {};
   w.q = (const uint16_t*)c.q; w.q_stride = c.q_stride;
   w.slab = slab; w.page_bytes = (int64_t)pool->page_bytes; w.tile_stride = pool->tile_stride; w.scales_off = scales_off;
-  w.lse = lse; w.saved = saved; w.weight_in = call.weight_in; w.weight_out = call.weight_out;
+  w.lse = lse; w.saved = saved; w.saved_stride = saved_stride; w.weight_in = call.weight_in; w.weight_out = call.weight_out;
   w.d = d; w.n_heads = H; w.s = sc;
   if (call.weight_in != call.weight_out) work.insert(work.end(), idle.begin(), idle.end());
-  const int per = saved ? 256 : 32;
+  const int per = saved ? 256 : kTile;
   for (size_t i = 0; i < work.size();) {
     w.n_users = 0; w.n_units = 0;
-    for (; i < work.size() && w.n_users < kScoredUsers; ++i) {
+    for (; i < work.size() && w.n_users < kTokenUsers; ++i) {
       const int units = (int)(((int64_t)work[i].keys + per - 1) / per);
       if (units == 0) continue;
       if (w.n_units > 0 && (int64_t)w.n_units + units >= 1 << 23) break;
@@ -214,14 +229,15 @@ int relaygr::scored8(KvPool* pool, const ScoredCall& call, hipStream_t st) {
     if (w.n_users == 0) break;
     const dim3 grid((unsigned)w.n_units);
     if (saved) {
-      if (c.softmax) hipLaunchKernelGGL((weigh8_saved_kernel<true, kScoredUsers>), grid, dim3(256), 0, st, w);
-      else hipLaunchKernelGGL((weigh8_saved_kernel<false, kScoredUsers>), grid, dim3(256), 0, st, w);
+      if (c.softmax) hipLaunchKernelGGL((weigh8_saved_kernel<true, kTokenUsers>), grid, dim3(256), 0, st, w);
+      else hipLaunchKernelGGL((weigh8_saved_kernel<false, kTokenUsers>), grid, dim3(256), 0, st, w);
     } else {
       by_head(cfg, [&](auto h, auto dim) {
         using HT = decltype(h);
         constexpr int DH = decltype(dim)::value;
-        if (c.softmax) hipLaunchKernelGGL((weigh8_kernel<HT, DH, true, kScoredUsers>), grid, dim3(kWeighWaves * 64), 0, st, w);
-        else hipLaunchKernelGGL((weigh8_kernel<HT, DH, false, kScoredUsers>), grid, dim3(kWeighWaves * 64), 0, st, w);
+        by_form([&](auto sm, auto bias) {
+          hipLaunchKernelGGL((weigh8_kernel<HT, DH, decltype(sm)::value, decltype(bias)::value, kTokenUsers>), grid, dim3(kWeighWaves * 64), 0, st, w);
+        });
       });
     }
     LAUNCH_CHECK(what);

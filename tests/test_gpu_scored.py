@@ -311,7 +311,8 @@ def test_weights_and_positions_beyond_4_gib():
     w = torch.full((far + 300,), -7.0, device=DEV)
     pos = torch.full((far + 300,), 1 << 20, dtype=torch.int32, device=DEV)
     pos[far:far + 200] = torch.arange(200, device=DEV, dtype=torch.int32)
-    want, near = c.call(bias=True, weigh=True)
+    want, near = c.call(bias=True, key_pos=[np.arange(200)], weigh=True)      # (the same, near)
+    c.check(want, near)
     scoring = rg.Scoring(slopes=dev(c.slopes, np.float32), key_position=pos, token_off=[far])
     out = rg.relaygr_cache_attend_scored(c.ctx, c.pool, 1, rg.KvRows(c.handles, c.row_off), c.q, scoring, weight_out=w)
     assert torch.equal(out, want) and torch.equal(w[far:far + 200], near[3:203])
