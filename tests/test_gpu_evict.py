@@ -134,6 +134,30 @@ def test_counts_ties_and_odd_weights(n):
     c.check(kept, [m], 0, n // 4)
 
 
+@pytest.mark.parametrize("n", [4095, 4096, 4097, 16385, 32768, 32769, 40001])
+def test_long_entries(n):
+    """Lengths around what the choosing holds in registers and in LDS: weights of many values and of few, whose ties lie in several spans of tokens; weights and positions over themselves."""
+    c = Case(128, 2, "fp16", [n], seed=n, layers=1, to_lens=[n])
+    rng = np.random.default_rng(n)
+    for few in (False, True):
+        mine = slice(c.token_off[0], c.token_off[0] + n)
+        c.w[mine] = rng.integers(0, 3, n) if few else np.exp(2 * rng.standard_normal(n))
+        for m, first, recent in ((n - 1, 4, 100), (n // 2, 0, 0), (n // 3, 5000 if n > 16384 else 1, 64)):
+            rows = rg.KvRows(c.handles, [0, m], key_len=[n])
+            weight, position = torch.from_numpy(c.w.copy()).to(DEV), torch.from_numpy(c.pos).to(DEV)
+            other = int(c.to[0])
+            kept = rg.relaygr_kv_pool_evict(c.pool, rows, weight, c.token_off, first, recent, to=[other], weight_out=weight, position=position, position_out=position,
+                                            out_off=c.token_off).cpu().numpy()
+            want = choose(c.w[mine], m, first, recent)
+            assert np.array_equal(kept, want), (few, m)
+            at = np.arange(n)[:m] + c.token_off[0]
+            expected_w, expected_pos = c.w.copy(), c.pos.copy()
+            expected_w[at], expected_pos[at] = c.w[mine][want], c.pos[mine][want]
+            assert np.array_equal(weight.cpu().numpy(), expected_w) and np.array_equal(position.cpu().numpy(), expected_pos)
+            for x, read in zip(c.kv[0], rg.relaygr_kv_pool_read(c.pool, 0, rg.KvRows([other], [0, m]))):
+                assert np.array_equal(read.double().cpu().numpy(), held(x[0][want], "fp16").reshape(m, 128))
+
+
 def test_many_users_and_what_lies_beside_them():
     """More users than a launch takes; other entries, and blocks behind what stays, keep every bit."""
     lens = [int(x) for x in np.random.default_rng(3).integers(1, 400, 150)]
