@@ -86,9 +86,9 @@ class ScoringC(C.Structure):
 
 
 class KvEvictionC(C.Structure):
-    _fields_ = [("first", C.c_int32), ("recent", C.c_int32), ("to", C.POINTER(C.c_uint64)), ("weight", C.c_void_p), ("position", C.c_void_p),
-                ("token_off", C.POINTER(C.c_int64)), ("kept", C.c_void_p), ("weight_out", C.c_void_p), ("position_out", C.c_void_p),
-                ("out_off", C.POINTER(C.c_int64))]
+    _fields_ = [("first", C.c_int32), ("recent", C.c_int32), ("to", C.c_void_p), ("weight", C.c_void_p), ("position", C.c_void_p),
+                ("token_off", C.c_void_p), ("kept", C.c_void_p), ("weight_out", C.c_void_p), ("position_out", C.c_void_p),
+                ("out_off", C.c_void_p)]
 
 
 class AdmissionParamsC(C.Structure):
@@ -556,13 +556,13 @@ def relaygr_rotary(cfg: ModelConfigC, rope: Rope, positions: torch.Tensor, q: to
             return relaygr_rotary(cfg, rope, positions, q, k, transposed, q_out, k_out)
     n = q.shape[0]
     pos = _vector("rotary: positions", positions, torch.int32, device, n)
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=device) if q_out is None else q_out
+    q_out = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else q_out
     qp, qs = _rotary_rows("rotary: q", cfg, n, device, q)
     qo, qos = _rotary_rows("rotary: q_out", cfg, n, device, q_out)
     kp = ko = None
     ks = kos = 0
     if k is not None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=device) if k_out is None else k_out
+        k_out = torch.empty_like(k, memory_format=torch.contiguous_format) if k_out is None else k_out
         kp, ks = _rotary_rows("rotary: k", cfg, n, device, k)
         ko, kos = _rotary_rows("rotary: k_out", cfg, n, device, k_out)
     _check(load_library().relaygr_rotary(C.byref(cfg), rope.ref, n, pos, int(transposed), qp, qs, qo, qos, kp, ks, ko, kos,
@@ -612,10 +612,12 @@ class Scoring:
                 raise RelayGRError(RELAYGR_EINVAL, f"Scoring: {name} of {a.size} users for a batch of {rows.n_users}")
 
 
-def _tokens_fit(what: str, rows: KvRows, lens, token_off: np.ndarray, t: Optional[torch.Tensor]) -> None:
-    """Refuses a tensor that does not hold the tokens of every user."""
-    if t is not None and rows.n_users and int((token_off + lens).max()) > t.numel():
-        raise RelayGRError(RELAYGR_EINVAL, f"{what}: {t.numel()} elements do not hold every user's tokens")
+def _tokens_fit(what: str, rows: KvRows, lens, token_off: np.ndarray, tensors) -> None:
+    """Refuses tensors, by name, of which one does not hold the tokens of every user."""
+    need = int((token_off + lens).max()) if rows.n_users else 0
+    for name, t in tensors:
+        if t is not None and need > t.numel():
+            raise RelayGRError(RELAYGR_EINVAL, f"{what}: {name} of {t.numel()} elements does not hold every user's tokens")
 
 
 def _lens(pool: KvPool, rows: KvRows):
@@ -639,9 +641,8 @@ def relaygr_cache_attend_scored(ctx: Context, pool: KvPool, layer: int, rows: Kv
     wi = _vector("cache_attend_scored: weight", weight, torch.float32, pool.slab.device)
     wo = _vector("cache_attend_scored: weight_out", weight_out, torch.float32, pool.slab.device)
     if scoring.token_off is not None and (weight_out is not None or scoring.key_position is not None):
-        lens = _lens(pool, rows)
-        for name, t in (("key_position", scoring.key_position), ("weight", weight), ("weight_out", weight_out)):
-            _tokens_fit("cache_attend_scored: " + name, rows, lens, scoring.token_off, t)
+        _tokens_fit("cache_attend_scored", rows, _lens(pool, rows), scoring.token_off,
+                    (("key_position", scoring.key_position), ("weight", weight), ("weight_out", weight_out)))
     out, op, os_ = _result_rows("cache_attend_scored: out", pool, rows, out)
     _check(load_library().relaygr_cache_attend_scored(ctx.handle, pool.handle, layer, rows.ref, int(causal), scoring.ref, qp, qs, op, os_, wi, wo,
                                                       torch._C._cuda_getCurrentRawStream(pool.slab.device.index)))
@@ -663,17 +664,15 @@ def relaygr_kv_pool_evict(pool: KvPool, rows: KvRows, weight: torch.Tensor, toke
     out_off = None if out_off is None else _host_vector("kv_pool_evict: out_off", out_off, np.int64, n)
     to = None if to is None else _host_vector("kv_pool_evict: to", to, np.uint64, n)
     kept = torch.empty(rows.n_rows, dtype=torch.int32, device=device) if kept is None else kept
-    e = KvEvictionC(first, recent, None if to is None else to.ctypes.data_as(C.POINTER(C.c_uint64)), _vector("kv_pool_evict: weight", weight, torch.float32, device),
-                    _vector("kv_pool_evict: position", position, torch.int32, device), token_off.ctypes.data_as(C.POINTER(C.c_int64)),
+    e = KvEvictionC(first, recent, None if to is None else to.ctypes.data, _vector("kv_pool_evict: weight", weight, torch.float32, device),
+                    _vector("kv_pool_evict: position", position, torch.int32, device), token_off.ctypes.data,
                     _vector("kv_pool_evict: kept", kept, torch.int32, device, rows.n_rows), _vector("kv_pool_evict: weight_out", weight_out, torch.float32, device),
                     _vector("kv_pool_evict: position_out", position_out, torch.int32, device),
-                    None if out_off is None else out_off.ctypes.data_as(C.POINTER(C.c_int64)))
-    lens = _lens(pool, rows)
-    for name, t in (("weight", weight), ("position", position)):
-        _tokens_fit("kv_pool_evict: " + name, rows, lens, token_off, t)
-    counts = np.diff(rows.row_off)
-    for name, t in (("weight_out", weight_out), ("position_out", position_out)):
-        _tokens_fit("kv_pool_evict: " + name, rows, counts, rows.row_off[:-1] if out_off is None else out_off, t)
+                    None if out_off is None else out_off.ctypes.data)
+    _tokens_fit("kv_pool_evict", rows, _lens(pool, rows), token_off, (("weight", weight), ("position", position)))
+    if weight_out is not None or position_out is not None:
+        starts = rows.row_off[:-1]
+        _tokens_fit("kv_pool_evict", rows, rows.row_off[1:] - starts, starts if out_off is None else out_off, (("weight_out", weight_out), ("position_out", position_out)))
     _check(load_library().relaygr_kv_pool_evict(pool.handle, rows.ref, C.byref(e), torch._C._cuda_getCurrentRawStream(device.index)))
     return kept
 

@@ -14,14 +14,13 @@ def eviction(**kw):
     e = dict(first=0, recent=0, weight=0x100000, position=0x200000, token_off=[0, 1000, 2000], kept=0x300000, weight_out=0x400000, position_out=0x500000, out_off=None, to=None) | kw
     keep = []
 
-    def ptr(x, dtype, ctype):
+    def ptr(x, dtype):
         if x is None:
             return None
-        a = np.array(x, dtype=dtype)
-        keep.append(a)
-        return a.ctypes.data_as(C.POINTER(ctype))
-    c = B.KvEvictionC(e["first"], e["recent"], ptr(e["to"], np.uint64, C.c_uint64), e["weight"], e["position"], ptr(e["token_off"], np.int64, C.c_int64), e["kept"], e["weight_out"],
-                      e["position_out"], ptr(e["out_off"], np.int64, C.c_int64))
+        keep.append(np.array(x, dtype=dtype))
+        return keep[-1].ctypes.data
+    c = B.KvEvictionC(e["first"], e["recent"], ptr(e["to"], np.uint64), e["weight"], e["position"], ptr(e["token_off"], np.int64), e["kept"], e["weight_out"],
+                      e["position_out"], ptr(e["out_off"], np.int64))
     c.keep = keep
     return c
 
