@@ -73,6 +73,7 @@ int relaygr::scored8(KvPool* pool, const ScoredCall& call, hipStream_t st) {
   std::vector<Work> work, idle;      // idle: users without rows, whose weights are passed on
   std::vector<AttendLen> lens;
   int most_rows = 0;
+  int64_t row_items = 0, row_tiles = 0;      // of 32 rows, and those times their tiles of keys
   for (int u = 0; u < r->n_users; ++u) {
     const int keys = r->key_len ? r->key_len[u] : entries[u].prefix_len, n = r->row_off[u + 1] - r->row_off[u];
     if (keys < 0 || keys > entries[u].prefix_len) return fail(RELAYGR_EINVAL, "%s: user %d: %d keys of an entry of %d tokens", what, u, keys, entries[u].prefix_len);
@@ -84,6 +85,8 @@ int relaygr::scored8(KvPool* pool, const ScoredCall& call, hipStream_t st) {
     work.push_back({u, n, keys, 1, prefix, (int)((most + kTile - 1) / kTile)});
     lens.push_back({n, (int)most});
     most_rows = std::max(most_rows, n);
+    row_items += (n + 31) / 32;
+    row_tiles += (int64_t)((n + 31) / 32) * work.back().tiles;
   }
   if (weigh) {
     // (two users adding to one token would race)
@@ -111,7 +114,12 @@ int relaygr::scored8(KvPool* pool, const ScoredCall& call, hipStream_t st) {
     lse = (float*)take(need);
   }
   AttendRule rule = attend_rule(lens, H, dh, c.n_cus);
-  const int item_rows = most_rows <= 16 ? 16 : 32;
+  // Items of 16 rows where there are no more, and where there is little to do, of which twice as many make a shorter chain: at most 16 tiles of 32 rows a CU, or, of rows that
+  // see from row_first on and so less than is known here, two items a CU.  17, 64 and 200 rows of one user over 2048, 2048 and 4096 tokens (1, 2 and 14 tiles a CU) take 8.8, 9.8 and 20.6 us
+  // with 16 rows to an item and 10.3, 11.5 and 20.9 with 32 at heads of 128, 8.3, 8.7 and 14.2 against 9.0, 9.5 and 15.1 at 64; 8 users' 200 rows with sessions 13.5 and 16.9; 8 users of
+  // 64 rows over 4096 (32 a CU) 18.8 and 19.3 at 64, 26.6 and 25.0 at 128; 16 of 200 over 4096 (224 a CU) 106 and 92.
+  const bool little = s.row_first ? row_items * H <= 2 * c.n_cus : row_tiles * H <= 16 * c.n_cus;
+  const int item_rows = most_rows <= 16 || little ? 16 : 32;
   const size_t row_bytes = (size_t)d * 4 + (c.softmax ? (size_t)H * 16 : 0);
   const auto items_of = [&](const Work& w) { return ((int64_t)w.rows + item_rows - 1) / item_rows * w.parts; };
   int64_t partial_rows = 0, most_items = 0;

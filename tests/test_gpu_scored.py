@@ -137,6 +137,20 @@ def test_long_histories_cut_along_the_keys(lens, rows, form):
 
 
 @pytest.mark.parametrize("form", ["silu", "softmax"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d,heads", [(256, 8), (512, 8), (1024, 8)])
+def test_kernels_of_few_and_of_many_rows_and_users(d, heads, dtype, form):
+    """Few users or many (with the distances' arrays or by place), of few rows each or of so many that items have 32."""
+    for lens, rows, check in (([1100] * 4, [330, 1, 300, 345], [0, 1, 3]), ([1000 + 7 * u for u in range(18)], [70 + u % 5 for u in range(18)], [0, 9, 17]),
+                              ([30 + 11 * u for u in range(20)], [1 + u % 12 for u in range(20)], None)):
+        c = Case(d, heads, dtype, form, lens, rows, seed=d + len(lens), check=check)
+        c.check(c.call(causal=True, cap=20.0, prefix=[5] * len(lens), window=600))
+        c.check(*c.call(bias=True, causal=True, weigh=True))
+        key_pos = [np.cumsum(c.rng.integers(1, 4, n)) for n in lens]
+        c.check(c.call(causal=True, cap=10.0, bias=True, key_pos=key_pos, row_pos=np.concatenate([k[-1] + 1 + np.arange(m) for k, m in zip(key_pos, rows)])))
+
+
+@pytest.mark.parametrize("form", ["silu", "softmax"])
 def test_launches_that_do_not_keep_the_codes(form):
     """Few rows over more than the caches hold."""
     lens, rows = [8200] * 66, [1] * 65 + [2]
