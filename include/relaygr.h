@@ -341,10 +341,10 @@ int  relaygr_rotary(const relaygr_model_config* cfg, const relaygr_rope* rope, i
  * and row i sees the first prefix[u] tokens, whatever else holds, and those in [first_i, end_i): end_i = key_len, causal rows key_len - n + 1 + i, and no more than
  * row_end[i]; first_i = 0, no less than row_first[i] (a session, a document), and no less than end_i - window if window > 0. */
 typedef struct {
-  float cap;                     /* 0: none */
+  float cap;                     /* 0: none; otherwise from 2^-100 to 2^100 */
   int32_t window;                /* 0: none */
   const float* slopes;           /* DEVICE [n_heads], or null: no bias */
-  const int32_t* prefix;         /* HOST [n_users], or null: 0 (more than key_len counts as key_len) */
+  const int32_t* prefix;         /* HOST [n_users], or null: 0 (more than key_len counts as key_len; fewer than 2^25) */
   const int32_t* row_first;      /* DEVICE [rows], or null */
   const int32_t* row_end;        /* DEVICE [rows], or null */
   const int32_t* row_position;   /* DEVICE [rows], or null */
@@ -355,7 +355,7 @@ typedef struct {
  * the tokens that row i sees; rows that see nothing are zero).  weight_out (DEVICE fp32, or null): what each token received, added up,
  *   weight_out[token_off[u] + j] = weight_in[token_off[u] + j] + sum over heads and rows of w_ij      (|w_ij| in the SiLU form; weight_in null: from 0)
  * for the first key_len[u] tokens of every user, in fp32 and in an order that the call's sizes and the context's scratch decide; weight_in may be weight_out.
- * RELAYGR_EINVAL if two users' tokens overlap there.  RELAYGR_ENOSPC if the scratch does not hold 4 n_heads bytes a row (softmax with weights). */
+ * RELAYGR_EINVAL if two users' tokens overlap there, or weight_in's and weight_out's otherwise.  RELAYGR_ENOSPC if the scratch does not hold 4 n_heads bytes a row (softmax with weights). */
 int  relaygr_cache_attend_scored(relaygr_ctx* ctx, relaygr_kv_pool* pool, int32_t layer, const relaygr_kv_rows* rows, int32_t causal,
                                  const relaygr_scoring* scoring, const void* q, int64_t q_stride, void* out, int64_t out_stride,
                                  const float* weight_in, float* weight_out, void* hip_stream);

@@ -28,7 +28,8 @@ int check_words(const char* name, const void* p) {
 }
 
 int check_scoring(const relaygr_kv_rows* r, const relaygr_scoring& s, const float* weight_in, const float* weight_out) {
-  if (!(s.cap >= 0) || !std::isfinite(s.cap)) return fail(RELAYGR_EINVAL, "%s: the cap is negative or not finite", what);
+  // (beyond these, the factors of a capped score leave fp32's range)
+  if (!(s.cap == 0 || (s.cap >= 0x1p-100f && s.cap <= 0x1p100f))) return fail(RELAYGR_EINVAL, "%s: a cap of %g is neither 0 nor between 2^-100 and 2^100", what, s.cap);
   if (s.window < 0) return fail(RELAYGR_EINVAL, "%s: window < 0", what);
   int rc;
   for (const auto& x : {std::pair<const char*, const void*>("slopes", s.slopes), {"row_first", s.row_first}, {"row_end", s.row_end}, {"row_position", s.row_position},
@@ -96,6 +97,16 @@ int relaygr::scored8(KvPool* pool, const ScoredCall& call, hipStream_t st) {
     std::sort(tokens.begin(), tokens.end());
     for (size_t i = 1; i < tokens.size(); ++i)
       if (tokens[i].first < tokens[i - 1].second) return fail(RELAYGR_EINVAL, "%s: two users' weights overlap", what);
+    // (and so would a token that is written where another's weight is read)
+    if (call.weight_in && call.weight_in != call.weight_out) {
+      const auto at = [&](const float* x, int64_t j) { return (uintptr_t)x + 4 * (uintptr_t)j; };
+      for (size_t i = 0, j = 0; i < tokens.size() && j < tokens.size();) {
+        const uintptr_t in = at(call.weight_in, tokens[i].second), out = at(call.weight_out, tokens[j].second);
+        if (at(call.weight_in, tokens[i].first) < out && at(call.weight_out, tokens[j].first) < in)
+          return fail(RELAYGR_EINVAL, "%s: weight_out overlaps weight_in elsewhere than token by token", what);
+        if (in < out) ++i; else ++j;
+      }
+    }
   }
   if (!work.empty()) {
     if ((rc = check_rows_array(what, "q", c.q, c.q_stride, d)) != RELAYGR_OK) return rc;

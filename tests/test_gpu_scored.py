@@ -237,6 +237,32 @@ def test_nan_reaches_the_rows_that_see_it_only(d, heads, dtype, form):
         assert bool(torch.isfinite(mine).all()) and bool((mine[:at + 1] == 0).all())
 
 
+@pytest.mark.parametrize("cap", [2.0 ** -100, 2.0 ** -60, 2.0 ** 60, 2.0 ** 100])
+@pytest.mark.parametrize("form", ["silu", "softmax"])
+def test_the_smallest_and_the_largest_caps(cap, form):
+    c = Case(256, 4, "bf16", form, [100, 300], [2, 40], seed=71)
+    out = c.call(cap=cap, causal=True)
+    c.check(out)
+    if cap > 1:      # far above every score: as without one (a score's scaling, the series' five roundings and the change of units are within the eight half steps beside its sum's)
+        c.args["cap"] = 0.0
+        c.check(out)
+
+
+def test_users_whose_weights_interleave():
+    """weight_out may lie between the users' parts of weight_in."""
+    c = Case(128, 4, "bf16", "softmax", [60, 50], [3, 2], seed=73)
+    plain = rg.Scoring(token_off=[0, 200])
+    rows = rg.KvRows(c.handles, c.row_off)
+    x = torch.rand(400, device=DEV)
+    want = rg.relaygr_cache_attend_scored(c.ctx, c.pool, 1, rows, c.q, plain, weight=x, weight_out=torch.empty(400, device=DEV))
+    apart = torch.empty(400, device=DEV)
+    rg.relaygr_cache_attend_scored(c.ctx, c.pool, 1, rows, c.q, plain, weight=x, weight_out=apart)
+    both = torch.cat([x, torch.zeros(100, device=DEV)])
+    assert torch.equal(rg.relaygr_cache_attend_scored(c.ctx, c.pool, 1, rows, c.q, plain, weight=both[:400], weight_out=both[100:]), want)
+    for o, n in ((0, 60), (200, 50)):
+        assert torch.equal(both[100 + o:100 + o + n], apart[o:o + n]) and torch.equal(both[o:o + n], x[o:o + n])
+
+
 def test_key_lengths_and_columns_of_wider_arrays():
     c = Case(256, 4, "bf16", "silu", [300, 200, 64], [20, 7, 3], seed=7)
     c.check(*c.call(key_len=[0, 130, 64], cap=8.0, bias=True, weigh=True))
@@ -356,23 +382,28 @@ def test_refusals():
     c = Case(256, 4, "bf16", "softmax", [100, 50], [2, 3], seed=59)
     good = dict(cap=1.0, slopes=dev(c.slopes, np.float32), token_off=c.token_off)
 
-    def code(scoring=None, weight=None, rows=None, pool=None, ctx=None, layer=1, **kw):
+    def code(scoring=None, weight=None, rows=None, pool=None, ctx=None, layer=1, weight_in=None, **kw):
         out = torch.full((5, 256), 3.0, dtype=torch.bfloat16, device=DEV)
         w = torch.full((c.n_tokens,), 3.0, device=DEV) if weight is None else weight
         rows = rg.KvRows(c.handles, c.row_off) if rows is None else rows
         with pytest.raises(rg.RelayGRError) as e:
-            rg.relaygr_cache_attend_scored(ctx or c.ctx, pool or c.pool, layer, rows, c.q, rg.Scoring(**(good if scoring is None else good | scoring)), out=out, weight_out=w, **kw)
+            rg.relaygr_cache_attend_scored(ctx or c.ctx, pool or c.pool, layer, rows, c.q, rg.Scoring(**(good if scoring is None else good | scoring)), out=out, weight=weight_in, weight_out=w, **kw)
         torch.cuda.synchronize()
         assert bool((out == 3.0).all()) and bool((w == 3.0).all())
         return e.value.code
     i32 = dict(dtype=torch.int32, device=DEV)
-    for s in (dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")), dict(window=-1), dict(prefix=[0, -1]), dict(prefix=[0]), dict(token_off=[0]), dict(token_off=[-1, 200]),
+    for s in (dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")), dict(cap=1e-31), dict(cap=2e30), dict(window=-1), dict(prefix=[0, -1]), dict(prefix=[0]), dict(token_off=[0]), dict(token_off=[-1, 200]),
               dict(token_off=[0, 99]), dict(token_off=[49, 0]), dict(token_off=[0, c.n_tokens - 49]), dict(slopes=torch.zeros(3, device=DEV)), dict(slopes=torch.zeros(4)),
               dict(slopes=torch.zeros(4, dtype=torch.float64, device=DEV)), dict(row_first=torch.zeros(4, **i32)), dict(row_end=torch.zeros(5, dtype=torch.int64, device=DEV)),
               dict(row_position=torch.zeros(10, **i32)[::2]), dict(key_position=torch.zeros(c.n_tokens - 20, **i32)), dict(row_end=torch.zeros(5, dtype=torch.int32))):
         assert code(scoring=s) == rg.RELAYGR_EINVAL, s
     assert code(weight=torch.full((c.n_tokens,), 3.0, dtype=torch.float16, device=DEV)) == rg.RELAYGR_EINVAL
     assert code(scoring=dict(token_off=None)) == rg.RELAYGR_EINVAL
+    # weights that are read where others are written
+    both = torch.full((2 * c.n_tokens,), 3.0, device=DEV)
+    for by in (1, 99, 104):
+        assert code(weight=both[by:by + c.n_tokens], weight_in=both[:c.n_tokens]) == rg.RELAYGR_EINVAL, by
+        assert code(weight=both[:c.n_tokens], weight_in=both[by:by + c.n_tokens]) == rg.RELAYGR_EINVAL, by
     assert code(layer=2) == rg.RELAYGR_EINVAL and code(rows=rg.KvRows([c.handles[0], 12345], [0, 2, 5], key_len=[100, 50])) == rg.RELAYGR_ENOENT
     assert code(rows=rg.KvRows(c.handles, [0, 2, 5], key_len=[101, 50])) == rg.RELAYGR_EINVAL
     assert code(ctx=context_for(model(512, 8, "bf16"), 1, 8)) == rg.RELAYGR_EINVAL
