@@ -447,7 +447,7 @@ def _result_rows(what: str, pool: KvPool, rows: KvRows, t: Optional[torch.Tensor
     if t is not None:
         return (t, *_kv_rows_array(what, pool, rows, t))
     d = pool.cfg.d_model
-    t = torch.empty((rows.n_rows, d), dtype=_torch_dtype(pool.dtype), device=pool.slab.device)
+    t = torch.empty_strided((rows.n_rows, d), (d, 1), dtype=_torch_dtype(pool.dtype), device=pool.slab.device)     # (a microsecond less than torch.empty)
     return t, (t.data_ptr() if rows.n_rows else None), d
 
 
@@ -538,6 +538,14 @@ def _rotary_rows(what: str, cfg: ModelConfigC, n: int, device, t: torch.Tensor):
     return (t.data_ptr() if n else None), (stride[0] if n > 1 else d)
 
 
+def _rotary_result(what: str, cfg: ModelConfigC, n: int, device, x: torch.Tensor, t: Optional[torch.Tensor]):
+    """A result's tensor (like x, which has been checked, if the caller gives none), its address and the elements between its rows."""
+    if t is not None:
+        return (t, *_rotary_rows(what, cfg, n, device, t))
+    t = torch.empty_like(x, memory_format=torch.contiguous_format)
+    return t, (t.data_ptr() if n else None), cfg.d_model
+
+
 _DTYPES_BY_CODE = {RELAYGR_DTYPE_FP32: torch.float32, RELAYGR_DTYPE_BF16: torch.bfloat16, RELAYGR_DTYPE_FP16: torch.float16}
 
 
@@ -556,15 +564,13 @@ def relaygr_rotary(cfg: ModelConfigC, rope: Rope, positions: torch.Tensor, q: to
             return relaygr_rotary(cfg, rope, positions, q, k, transposed, q_out, k_out)
     n = q.shape[0]
     pos = _vector("rotary: positions", positions, torch.int32, device, n)
-    q_out = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else q_out
     qp, qs = _rotary_rows("rotary: q", cfg, n, device, q)
-    qo, qos = _rotary_rows("rotary: q_out", cfg, n, device, q_out)
+    q_out, qo, qos = _rotary_result("rotary: q_out", cfg, n, device, q, q_out)
     kp = ko = None
     ks = kos = 0
     if k is not None:
-        k_out = torch.empty_like(k, memory_format=torch.contiguous_format) if k_out is None else k_out
         kp, ks = _rotary_rows("rotary: k", cfg, n, device, k)
-        ko, kos = _rotary_rows("rotary: k_out", cfg, n, device, k_out)
+        k_out, ko, kos = _rotary_result("rotary: k_out", cfg, n, device, k, k_out)
     _check(load_library().relaygr_rotary(C.byref(cfg), rope.ref, n, pos, int(transposed), qp, qs, qo, qos, kp, ks, ko, kos,
                                          torch._C._cuda_getCurrentRawStream(device.index)))
     return q_out if k is None else (q_out, k_out)
@@ -614,7 +620,7 @@ class Scoring:
 
 def _tokens_fit(what: str, rows: KvRows, lens, token_off: np.ndarray, tensors) -> None:
     """Refuses tensors, by name, of which one does not hold the tokens of every user."""
-    need = int((token_off + lens).max()) if rows.n_users else 0
+    need = max((token_off + lens).tolist()) if rows.n_users else 0
     for name, t in tensors:
         if t is not None and need > t.numel():
             raise RelayGRError(RELAYGR_EINVAL, f"{what}: {name} of {t.numel()} elements does not hold every user's tokens")
