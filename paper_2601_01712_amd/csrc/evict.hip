@@ -113,7 +113,11 @@ int evict(KvPool* pool, const relaygr_kv_rows* r, const relaygr_kv_eviction* e, 
     if (p.n_users == 0) break;
     hipLaunchKernelGGL(evict_choose_kernel, dim3((unsigned)p.n_users), dim3(kChooseThreads), 0, st, p);
     by_head(cfg, [&](auto h, auto dim) {
-      hipLaunchKernelGGL((evict_move_kernel<decltype(h), decltype(dim)::value>), dim3((unsigned)(p.n_units * of_group)), dim3(kMoveWaves * 64), 0, st, p);
+      using HT = decltype(h);
+      constexpr int DH = decltype(dim)::value, WIDE = kWideWaves<DH>;
+      const dim3 grid((unsigned)(p.n_units * of_group));
+      if (in_place && grid.x <= kWideGroups) hipLaunchKernelGGL((evict_move_kernel<HT, DH, WIDE>), grid, dim3(WIDE * 64), 0, st, p);
+      else hipLaunchKernelGGL((evict_move_kernel<HT, DH, kMoveWaves>), grid, dim3(kMoveWaves * 64), 0, st, p);
     });
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return fail(RELAYGR_EHIP, "launch %s: %s", what, hipGetErrorString(err));

@@ -222,16 +222,20 @@ __device__ __forceinline__ uint32_t quad_transpose(uint32_t w, uint32_t sel1, ui
   return __builtin_amdgcn_perm(w, y, sel2);
 }
 
-// Moving: a wavefront to a tile of one head of K or of V, a workgroup to kMoveWaves of them, one behind the other, and a lane to a token: K's features of one are 16-byte pieces, V's are
+// Moving: a wavefront to a tile of one head of K or of V, a workgroup to WAVES of them, one behind the other, and a lane to a token: K's features of one are 16-byte pieces, V's are
 // bytes of tiles that go to LDS, two at a time, and the tile that is written goes by way of it too, after words have changed from four features of a token to four tokens of a feature.
 // In place a workgroup takes all the tiles of its head one group after the other: what a group reads are tiles from its first on, which the groups before it have left
 // alone, and its wavefronts write only when all of them have read.  32 users of 151 316 tokens, three quarters of which stay, of a width of 512 in two layers elsewhere: 107 us,
 // 5.1 TB/s (a byte at a time from V's tiles where they lie in memory, with the words in scratch: 242); one user's 4095 tokens of a width of 256 6.2 us.
-constexpr int kMoveWaves = 4;
-template <typename H, int DH>
-__global__ __launch_bounds__(kMoveWaves * 64) void evict_move_kernel(EvictParams p) {
+// In place, and in few workgroups (of a user's heads, K and V, and layers), those are as wide as the registers and LDS allow: us, four wavefronts / 16 (eight at heads of 128), three quarters stay in two
+// layers: one user of 16 384 tokens, d = 512 186 / 112 (elsewhere 40), 8 of 4096 54.5 / 39.8 (34), 16 (512 workgroups) 65.6 / 62.6, 32 103 / 112 (106); d = 1024, 8 84 / 68, 16 (512) 113 / 120; d = 256,
+// 32 users of 1000 and four heads (512) 23.4 / 24.1, 64 32 / 40.
+constexpr int kMoveWaves = 4, kWideGroups = 512;
+template <int DH> constexpr int kWideWaves = DH == 128 ? 8 : 16;
+template <typename H, int DH, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void evict_move_kernel(EvictParams p) {
   constexpr int BLOCK = kTile * DH, CHUNKS = DH / 16, KP = DH / 32, WORDS = DH / 4, SLOTS = 2;
-  __shared__ __attribute__((aligned(16))) uint8_t turn[kMoveWaves][SLOTS * BLOCK];
+  __shared__ __attribute__((aligned(16))) uint8_t turn[WAVES][SLOTS * BLOCK];
   const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int of_group = p.n_layers * p.n_heads * 2;
@@ -245,7 +249,7 @@ __global__ __launch_bounds__(kMoveWaves * 64) void evict_move_kernel(EvictParams
   const char* from = p.slab + u.from * p.page_bytes;
   char* to = p.slab + u.to * p.page_bytes;
   uint8_t* lds = turn[wave];
-  for (int t0 = (group - u.unit0) * kMoveWaves;; t0 += kMoveWaves) {
+  for (int t0 = (group - u.unit0) * WAVES;; t0 += WAVES) {
     const int t = t0 + wave;
     const bool mine = t < tiles;
     u32x4_t x[CHUNKS];
@@ -338,7 +342,7 @@ __global__ __launch_bounds__(kMoveWaves * 64) void evict_move_kernel(EvictParams
       for (int c = 0; c < CHUNKS; ++c) *reinterpret_cast<u32x4_t*>(at + (is_v ? c * 1024 + lane * 16 : g * (KP * 1024) + (c >> 1) * 1024 + (c & 1) * 512 + l32 * 16)) = x[c];
       if (lane == 0) *reinterpret_cast<float*>(tile + scale_off) = scale;
     }
-    if (!p.in_place || t0 + kMoveWaves >= tiles) break;
+    if (!p.in_place || t0 + WAVES >= tiles) break;
   }
 }
 

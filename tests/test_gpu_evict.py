@@ -158,6 +158,17 @@ def test_long_entries(n):
                 assert np.array_equal(read.double().cpu().numpy(), held(x[0][want], "fp16").reshape(m, 128))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d,heads", [(256, 8), (512, 8), (1024, 8)])
+def test_in_place_by_few_and_by_many_workgroups(d, heads, dtype):
+    """Histories of many tiles, a few of them and so many that the launch takes narrower workgroups."""
+    for lens in ([5000, 1030], [int(n) for n in np.random.default_rng(d).integers(300, 700, 18)]):
+        for of in (0.3, 0.97):
+            keep = [int(of * n) for n in lens]
+            c = Case(d, heads, dtype, lens, seed=d, layers=2)
+            c.check(c.evict(keep, 2, 50), keep, 2, 50)
+
+
 def test_many_users_and_what_lies_beside_them():
     """More users than a launch takes; other entries, and blocks behind what stays, keep every bit."""
     lens = [int(x) for x in np.random.default_rng(3).integers(1, 400, 150)]

@@ -42,7 +42,7 @@ def test_attention_reads_its_work_item_by_scalar_loads(tmp_path, instance):
     assert re.search(r"global_load_dwordx4 v\[\d+:\d+\], v\d+, s\[", start)
 
 
-@pytest.mark.parametrize("header,instance", [("evict8.h", "relaygr::evict_move_kernel<Bf16, 64>(EvictParams)"),
+@pytest.mark.parametrize("header,instance", [("evict8.h", "relaygr::evict_move_kernel<Bf16, 64, 16>(EvictParams)"),
                                              ("scored8.h", "relaygr::scored8_few_kernel<Bf16, 64, true, true, true, 128>(ScoredParams<128>)"),
                                              ("scored8.h", "relaygr::scored8_kernel<Bf16, 64, false, true, 16>(ScoredParams<16>)")])
 def test_no_scratch(tmp_path, header, instance):
