@@ -598,23 +598,26 @@ class Scoring:
         self.token_off = None if token_off is None else _host_vector("Scoring: token_off", token_off, np.int64)
         if key_position is not None and token_off is None:
             raise RelayGRError(RELAYGR_EINVAL, "Scoring: key_position without token_off")
-        self.tensors = [("slopes", slopes, torch.float32), ("row_first", row_first, torch.int32), ("row_end", row_end, torch.int32),
-                        ("row_position", row_position, torch.int32), ("key_position", key_position, torch.int32)]
+        self.tensors = [x for x in (("slopes", slopes, torch.float32), ("row_first", row_first, torch.int32), ("row_end", row_end, torch.int32),
+                                    ("row_position", row_position, torch.int32), ("key_position", key_position, torch.int32)) if x[1] is not None]
+        self.arrays = [x for x in (("prefix", self.prefix), ("token_off", self.token_off)) if x[1] is not None]
         self.c = ScoringC(cap, window, None, None if self.prefix is None else self.prefix.ctypes.data_as(C.POINTER(C.c_int32)), None, None, None, None,
                           None if self.token_off is None else self.token_off.ctypes.data_as(C.POINTER(C.c_int64)))
         self.ref = C.byref(self.c)
+
+    def __setattr__(self, name, value):
+        if "ref" in self.__dict__ and value is not self.__dict__.get(name):     # (made: the struct has its values)
+            raise AttributeError(f"Scoring: {name} cannot be replaced; change arrays in place, or make another")
+        object.__setattr__(self, name, value)
 
     def bind(self, pool: KvPool, rows: KvRows) -> None:
         """Checks the arrays against a batch and puts the tensors' addresses into the struct."""
         device = pool.slab.device
         for name, t, dtype in self.tensors:
-            if t is None:
-                continue
             n = pool.cfg.n_heads if name == "slopes" else None if name == "key_position" else rows.n_rows
             setattr(self.c, name, _vector("Scoring: " + name, t, dtype, device, n))
-        for name in ("prefix", "token_off"):
-            a = getattr(self, name)
-            if a is not None and a.size != rows.n_users:
+        for name, a in self.arrays:
+            if a.size != rows.n_users:
                 raise RelayGRError(RELAYGR_EINVAL, f"Scoring: {name} of {a.size} users for a batch of {rows.n_users}")
 
 

@@ -94,16 +94,26 @@ struct TileRange {
     return b <= pre || (b <= all_hi && a >= all_from);
   }
 };
-__device__ __forceinline__ TileRange tile_range(const RowRange& r, bool is_row) {
-  const bool any = is_row && r.hi > r.lo;
+__device__ __forceinline__ TileRange tile_range(const Scoring& s, const ScoredUser& u, int row0, int rows, const RowRange& r, bool is_row) {
   TileRange t;
-  t.pre = __builtin_amdgcn_readfirstlane(r.pre);      // (the same for all rows of a user)
+  t.pre = u.prefix();
   t.pre_tiles = (t.pre + kTile - 1) / kTile;
-  const int hi = wave_max_i32(any ? r.hi : 0);
-  t.t0 = max(wave_min_i32(any ? r.lo : 0x7FFFFFFF) / kTile, t.pre_tiles);
+  int lo, hi;
+  if (!s.row_first && !s.row_end) {      // ranges climb with the rows: scalar work, of the first and the last
+    const RowRange a = row_range(s, u, row0), b = row_range(s, u, row0 + rows - 1);
+    lo = a.lo;
+    hi = b.hi > b.lo ? b.hi : 0;
+    t.all_from = b.from();
+    t.all_hi = a.hi;
+  } else {
+    const bool any = is_row && r.hi > r.lo;
+    hi = wave_max_i32(any ? r.hi : 0);
+    lo = wave_min_i32(any ? r.lo : 0x7FFFFFFF);
+    t.all_from = wave_max_i32(is_row ? r.from() : 0);
+    t.all_hi = wave_min_i32(is_row ? r.hi : 0x7FFFFFFF);
+  }
+  t.t0 = max(lo / kTile, t.pre_tiles);
   t.n = t.pre_tiles + max((hi + kTile - 1) / kTile - t.t0, 0);
-  t.all_from = wave_max_i32(is_row ? r.from() : 0);
-  t.all_hi = wave_min_i32(is_row ? r.hi : 0x7FFFFFFF);
   return t;
 }
 
@@ -315,6 +325,7 @@ __device__ __forceinline__ void scored8_join_last(const ScoredParams<USERS>& p, 
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      if (r0 + 4 * i >= it.n_rows) break;      // (the same for all lanes)
       ScoredSum<SOFTMAX>& a = sum[i];
 #pragma unroll
       for (int by = LANES; by < 64; by *= 2) {
@@ -488,7 +499,7 @@ __global__ __launch_bounds__(kAttendWaves * 64, DH == 128 ? 2 : 3) void scored8_
   const int place_of = BIAS ? row_place(p.s, u, i_row) : 0;
   Bias bias = {};
   if constexpr (BIAS) bias = bias_of(p.s, u, head, it.first_row, it.n_rows, place_of);
-  const TileRange tiles = tile_range(range, is_row);
+  const TileRange tiles = tile_range(p.s, u, it.first_row, it.n_rows, range, is_row);
   const int v0 = (int)((int64_t)it.piece * tiles.n / u.parts()), v1 = (int)((int64_t)(it.piece + 1) * tiles.n / u.parts());
 
   f32x16_t oacc[DB];
@@ -645,7 +656,7 @@ __global__ __launch_bounds__(kAttendWaves * 64, DH == 128 ? 2 : 4) void scored8_
   const int place_of = BIAS ? row_place(p.s, u, i_row) : 0;
   Bias bias = {};
   if constexpr (BIAS) bias = bias_of(p.s, u, head, it.first_row, it.n_rows, place_of);
-  const TileRange tiles = tile_range(range, is_row);
+  const TileRange tiles = tile_range(p.s, u, it.first_row, it.n_rows, range, is_row);
   const int v0 = (int)((int64_t)it.piece * tiles.n / u.parts()), v1 = (int)((int64_t)(it.piece + 1) * tiles.n / u.parts());
 
   f32x4_t oacc[FB];

@@ -99,3 +99,13 @@ def test_the_reference_of_the_gpu_tests():
 def test_host_arrays_are_vectors(kw):
     with pytest.raises(rg.RelayGRError):
         rg.Scoring(**kw)
+
+
+def test_scoring_is_what_it_was_made_with():
+    s = rg.Scoring(cap=2.0, prefix=[1, 2], token_off=[0, 10])
+    for name, value in (("prefix", [3, 4]), ("row_first", None if s.row_first is not None else np.zeros(2)), ("window", 5)):
+        with pytest.raises(AttributeError):
+            setattr(s, name, value)
+    s.prefix[:] = 7
+    s.token_off += 1
+    assert list(s.c.prefix[:2]) == [7, 7] and list(s.c.token_off[:2]) == [1, 11]
