@@ -886,7 +886,7 @@ __global__ __launch_bounds__(256) void weigh8_saved_kernel(WeighParams<USERS> p)
     for (int k = 0; k < 8; ++k)
       if (h0 + k < p.n_heads) sum += weight_of<SOFTMAX>(of[k] - (SOFTMAX ? lse[k] : 0.f), inv);
   };
-  load(0, x[0]);
+  if (n > 0) load(0, x[0]);      // (users without rows have no scores)
   for (int i = 0; i < n; i += 2) {
     if (i + 1 < n) load(i + 1, x[1]);
     add(i, x[0]);
