@@ -191,6 +191,14 @@ def test_idle_users_pass_their_weights_on():
     assert torch.equal(after[mine], before[mine]) and bool((after[~mine] == -7.0).all())
 
 
+@pytest.mark.parametrize("form", ["silu", "softmax"])
+@pytest.mark.parametrize("rows", [[2, 0, 3, 0], [0, 40, 0, 0]])
+def test_idle_users_among_others(rows, form):
+    """Users without rows, of longer histories than the others and behind them, beside scores that are kept (few rows) or not."""
+    c = Case(128, 4, "bf16", form, [100, 500, 70, 900], rows, seed=79)
+    c.check(*c.call(causal=True, cap=9.0, weigh=True))
+
+
 def test_large_scores_infinities_and_caps():
     """Scores beyond exp's range, with a cap that brings them back; rows of infinities and NaN are those rows' own."""
     c = Case(128, 4, "bf16", "softmax", [200, 90], [33, 5], seed=5)
