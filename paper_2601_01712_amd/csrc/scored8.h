@@ -898,8 +898,8 @@ __global__ __launch_bounds__(256) void weigh8_saved_kernel(WeighParams<USERS> p)
 }
 
 // From K and q again: a workgroup to a tile, whose wavefronts share the user's (head, row block) pairs and add up over them in registers; the next pair's rows are on their
-// way while one is worked on.  What bounds it is the vector ALU, 14 instructions a score: 32 users of 200 to 1000 rows over about 4096 keys, d = 512, cap and bias (561 M scores) 336 us, the ALU
-// issuing in 87 % of the units' cycles; eight wavefronts a workgroup took 456 where four took 394.
+// way while one is worked on.  What bounds it is the vector ALU, 14 instructions a score: 32 users of 200 to 1000 rows over about 4096 keys, d = 512, cap and bias (561 M scores) 278 us, the users
+// of most rows first (334 in another order, the ALU issuing in 87 % of the units' cycles); eight wavefronts a workgroup took 456 where four took 394.
 constexpr int kWeighWaves = 4;
 template <typename H, int DH, bool SOFTMAX, bool BIAS, int USERS>
 __global__ __launch_bounds__(kWeighWaves * 64, DH == 128 ? 2 : 3) void weigh8_kernel(WeighParams<USERS> p) {
