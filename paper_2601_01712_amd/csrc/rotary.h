@@ -14,7 +14,7 @@
 namespace relaygr {
 
 constexpr int kRotaryPairs = 64;
-enum RotaryUnit { kRotaryHalf, kRotaryInterleaved, kRotaryOdd };     // what a lane takes: two chunks half the pairs apart; a chunk; a chunk whose partners are not a chunk
+enum RotaryUnit { kRotaryHalf, kRotaryLanes, kRotaryInterleaved, kRotaryOdd };     // what a lane takes: two chunks half the pairs apart; a chunk whose partners are another lane's; a chunk; a chunk whose partners are not a chunk
 struct RotaryArray { const char* in; char* out; int64_t in_stride, out_stride; };      // bytes between rows; in null: there is none
 struct RotaryParams {
   RotaryArray x[2];
@@ -66,7 +66,7 @@ template <> struct RotaryType<F16> : RotaryType16<F16> {};
 
 // A lane's unit of a row, in `heads_per` heads of every array: the angles are worked out once for all of them, while the first four heads are on their way.  A head's lanes are in
 // one wavefront and read all that they turn before they write any of it, so that `out` may be `in`.  What bounds it is HBM, or the launch: q and k of 65 536 rows of 512 bf16, 268 MB,
-// 59 us (4.5 TB/s; a copy of 1 GiB reaches 5.0), of 16 384 15.7; one row 3.8.
+// 53 us (5.1 TB/s; a copy of 1 GiB reaches 5.0), of 16 384 15.9; one row 3.8.
 template <class T, RotaryUnit UNIT>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   using R = RotaryType<T>;
@@ -79,6 +79,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   if (row >= p.n_rows || unit >= units) return;
   const bool turns = unit < turned;
   const int f0 = UNIT == kRotaryHalf && !turns ? p.dim + (unit - turned) * E : unit * E;
+  const int lane = threadIdx.x & 63, partner = !turns ? lane : f0 < half ? lane + half / E : lane - half / E;      // (kRotaryLanes: a row's lanes are side by side)
   const int head0 = blockIdx.y * p.heads_per, head1 = min(head0 + p.heads_per, p.n_heads);
   const int head_bytes = p.dh * BYTES;
   const int of_array = (head1 - head0 + AT_ONCE - 1) / AT_ONCE, batches = p.x[1].in ? 2 * of_array : of_array;
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
       const int f = f0 + i;
       if (UNIT != kRotaryHalf && f >= p.dim) continue;
       if (UNIT == kRotaryInterleaved && (i & 1)) { cs[i] = cs[i - 1]; sn[i] = -sn[i - 1]; continue; }
-      const int pair = UNIT == kRotaryInterleaved ? f >> 1 : UNIT == kRotaryOdd && f >= half ? f - half : f;
+      const int pair = UNIT == kRotaryInterleaved ? f >> 1 : UNIT != kRotaryHalf && f >= half ? f - half : f;
       float s, c;
       sincos_turns((uint32_t)((at * p.turns[pair]) >> 32), &s, &c);
       s = p.transposed ? -s : s;
@@ -125,12 +126,17 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   auto turn = [&](int batch, int slot) {
     const RotaryArray& x = p.x[batch >= of_array];
     const int h0 = head0 + (batch >= of_array ? batch - of_array : batch) * AT_ONCE;
-    if (!turns && x.in == x.out) return;
+    if (UNIT != kRotaryLanes && !turns && x.in == x.out) return;
     char* out = x.out + row * x.out_stride + f0 * BYTES;
 #pragma unroll
     for (int j = 0; j < AT_ONCE; ++j) {
       if (h0 + j >= head1) break;
       char* at = out + (int64_t)(h0 + j) * head_bytes;
+      u32x4_t other;
+      if constexpr (UNIT == kRotaryLanes) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) other[i] = (uint32_t)__shfl((int)w[slot][j][0][i], partner, 64);
+      }
       if (!turns) { *reinterpret_cast<u32x4_t*>(at) = w[slot][j][0]; continue; }
       float u[E], v[E], y[E];
       R::up(w[slot][j][0], u);
@@ -141,6 +147,11 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
         for (int i = 0; i < E; ++i) { y[i] = fmaf(u[i], cs[i], v[i] * sn[i]); z[i] = fmaf(v[i], cs[i], -u[i] * sn[i]); }
         *reinterpret_cast<u32x4_t*>(at) = R::down(y);
         *reinterpret_cast<u32x4_t*>(at + half * BYTES) = R::down(z);
+      } else if constexpr (UNIT == kRotaryLanes) {
+        R::up(other, v);
+#pragma unroll
+        for (int i = 0; i < E; ++i) y[i] = fmaf(u[i], cs[i], v[i] * sn[i]);
+        *reinterpret_cast<u32x4_t*>(at) = R::down(y);
       } else {
 #pragma unroll
         for (int i = 0; i < E; ++i) y[i] = fmaf(u[i], cs[i], (UNIT == kRotaryOdd ? odd[slot][j][i] : u[i ^ 1]) * sn[i]);

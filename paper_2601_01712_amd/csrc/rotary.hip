@@ -39,13 +39,19 @@ extern "C" int relaygr_rope_init(relaygr_rope* out, int32_t dim, int32_t layout,
 
 namespace {
 
+// Halves of pairs that are pieces of a cache line (fewer than 128 bytes): a lane takes both, each of 16 bytes, or one of them and its partners from another lane, so that lines are read and written whole.
+// That costs twice the angles and a turn by way of the lanes, and is for what the caches do not hold.  us, both / one (q and k, read and written): halves of 64 bytes, 65 536 rows of 512 bf16
+// (268 MB) 59.4 / 52.6, of 256 fp32 59.7 / 50.5, of 256 bf16 (134 MB) 27.6 / 29.4, 2048 of 512 5.4 / 5.9; of 32 bytes, 65 536 of 256 36.1 / 29.1, 16 384 (34 MB) 11.9 / 10.4, 4700 (10 MB) 6.9 / 6.9.
+bool by_lanes(int half_bytes, int64_t bytes) { return half_bytes < 128 && bytes >= (half_bytes < 64 ? (int64_t)16 << 20 : (int64_t)192 << 20); }
+
 // Lanes take all heads of a row while that leaves the chip enough of them: the angles are a lane's first work, some 25 instructions each, and rows that are read and written
 // whole are what the memory likes.  us, eight heads a lane / four (q and k of 8 heads): 65 536 rows of 512 bf16 59.0 / 64.4, of 1024 fp32 224 / 283; 16 384 rows (131 072 lanes at
 // eight) of 1024 bf16 28.9 / 25.2, of 512 fp32 28.4 / 25.0; four a lane / one: 2048 rows of 512 bf16 6.1 / 5.4, 4700 10.9 / 8.6.
 template <class T>
 void launch_rotary(RotaryParams p, hipStream_t st) {
   constexpr int E = RotaryType<T>::E;
-  const RotaryUnit unit = p.units_sh == 0 ? kRotaryInterleaved : (p.dim / 2) % E ? kRotaryOdd : kRotaryHalf;      // (units_sh carries the layout here)
+  const int64_t bytes = (int64_t)p.n_rows * p.n_heads * p.dh * (16 / E) * (p.x[1].in ? 4 : 2);      // read and written
+  const RotaryUnit unit = p.units_sh == 0 ? kRotaryInterleaved : (p.dim / 2) % E ? kRotaryOdd : by_lanes(p.dim / 2 * (16 / E), bytes) ? kRotaryLanes : kRotaryHalf;      // (units_sh carries the layout here)
   const int units = unit == kRotaryHalf ? p.dim / 2 / E + (p.dh - p.dim) / E : p.dh / E;
   p.units_sh = 0;
   while (1 << p.units_sh < units) ++p.units_sh;
@@ -58,6 +64,7 @@ void launch_rotary(RotaryParams p, hipStream_t st) {
     const dim3 grid((unsigned)((((int64_t)p.n_rows << p.units_sh) + 255) / 256), (unsigned)((p.n_heads + p.heads_per - 1) / p.heads_per));
     switch (unit) {
       case kRotaryHalf: hipLaunchKernelGGL((rotary_kernel<T, kRotaryHalf>), grid, dim3(256), 0, st, p); break;
+      case kRotaryLanes: hipLaunchKernelGGL((rotary_kernel<T, kRotaryLanes>), grid, dim3(256), 0, st, p); break;
       case kRotaryInterleaved: hipLaunchKernelGGL((rotary_kernel<T, kRotaryInterleaved>), grid, dim3(256), 0, st, p); break;
       default: hipLaunchKernelGGL((rotary_kernel<T, kRotaryOdd>), grid, dim3(256), 0, st, p); break;
     }

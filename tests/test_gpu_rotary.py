@@ -65,6 +65,26 @@ def test_whole_parts_and_odd_parts_of_heads(d, heads, dtype, layout, transposed)
                 assert torch.equal(g.cpu().view(n, heads, dh)[..., dim:], raw.view(n, heads, dh)[..., dim:]), "features behind the turned ones"
 
 
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("d,heads,dtype,n,dims", [(512, 8, "bf16", 100000, (64, 48, 32)), (256, 8, "fp16", 20000, (32, 16)), (256, 8, "fp32", 100000, (32, 16, 8)), (128, 1, "bf16", 260000, (96, 64))])
+def test_more_rows_than_the_caches_hold(d, heads, dtype, n, dims, transposed):
+    """Launches whose lanes take one half of each pair: the same numbers as of the same rows in small calls, which other tests hold to the formula."""
+    cfg = rg.make_config(2, d, heads, dtype)
+    gen = torch.Generator(DEV).manual_seed(d)
+    q, k = (torch.randn(n, d, generator=gen, device=DEV).to(TORCH[dtype]) for _ in range(2))
+    pos = torch.randint(-9000, 9000, (n,), generator=gen, device=DEV, dtype=torch.int32)
+    for dim in dims:
+        rope = rg.Rope(dim, gain=1.25)
+        got_q, got_k = rg.relaygr_rotary(cfg, rope, pos, q, k, transposed=transposed)
+        for at in (0, 4096, n - 3000):
+            r = slice(at, at + 3000)
+            want_q, want_k = rg.relaygr_rotary(cfg, rope, pos[r], q[r], k[r], transposed=transposed)
+            assert torch.equal(got_q[r], want_q) and torch.equal(got_k[r], want_k), (dim, at)
+        both = torch.cat([q, k], dim=1)      # in place, in rows of a wider array
+        rg.relaygr_rotary(cfg, rope, pos, both[:, :d], both[:, d:], transposed=transposed, q_out=both[:, :d], k_out=both[:, d:])
+        assert torch.equal(both[:, :d], got_q) and torch.equal(both[:, d:], got_k)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_far_and_negative_positions_scaled_frequencies_and_gain(dtype):
     d, heads, dh = 256, 4, 64
