@@ -475,9 +475,9 @@ __device__ __forceinline__ void scored8_store(const ScoredParams<USERS>& p, cons
 }
 
 // One item of up to 32 rows, as attend8_kernel: the workgroup's wavefronts take its tiles in turn, each straight from memory to its registers.  What bounds it is the vector ALU: 14
-// instructions a score with a cap and a bias, of which two exp and a reciprocal.  16 users of 512 rows over 4096 keys, d = 512, SiLU form, bias by positions 109 us (0.63 PFLOP/s,
-// the ALU issuing in 85 % of the units' cycles; relaygr_cache_attend's kernel 94); 32 of 200 to 1000 over about 4096, softmax, cap and bias 281 (94 %); 16 of 200 that see 2016 of 8192, d = 1024,
-// cap 57 (63 %, MFMAs 27 %).  Three wavefronts a SIMD at d_head 64 and two at 128 are what the registers hold; 64 rows an item spill: 395 us for the 357 that the second took then.
+// instructions a score with a cap and a bias, of which two exp and a reciprocal.  16 users of 512 rows over 4096 keys, d = 512, SiLU form, bias by positions 106 us (0.65 PFLOP/s,
+// the ALU issuing in 85 % of the units' cycles; relaygr_cache_attend's kernel 94); 32 of 200 to 1000 over about 4096, softmax, cap and bias 277 (95 %); 16 of 200 that see 2016 of 8192, d = 1024,
+// cap 56 (63 %, MFMAs 27 %).  Three wavefronts a SIMD at d_head 64 and two at 128 are what the registers hold; 64 rows an item spill (the second 395 us where 32 took 357).
 template <typename H, int DH, bool SOFTMAX, bool BIAS, int USERS>
 __global__ __launch_bounds__(kAttendWaves * 64, DH == 128 ? 2 : 3) void scored8_kernel(ScoredParams<USERS> p) {
   constexpr int KS = DH / 16, KP = DH / 32, DB = DH / 32;
@@ -630,7 +630,7 @@ __global__ __launch_bounds__(kAttendWaves * 64, DH == 128 ? 2 : 3) void scored8_
 //     (d_head 32: a chunk's halves are lanes' 8 bytes)
 //   V: the chunk of feature l16 of 16, token half kb, lane half g holds these very tokens, the first eight bytes those of T = 0, 1
 // What bounds it is HBM, or for single rows the chain of loads: 128 users of one row over 8192 keys, d = 512, bias, 162 us (1.07 GB, 6.7 TB/s), 201 with the scores
-// kept, whose 33.5 MB cost the same in whatever pieces they are stored; one row over 2048, d = 256, 9.1.
+// kept, whose 33.5 MB cost the same in whatever pieces they are stored; one row over 2048, d = 256, 8.2.
 template <typename H, int DH, bool SOFTMAX, bool BIAS, bool ONCE, int USERS>
 __global__ __launch_bounds__(kAttendWaves * 64, DH == 128 ? 2 : 4) void scored8_few_kernel(ScoredParams<USERS> p) {
   constexpr int KP = DH / 32, FB = DH / 16, KL = DH < 64 ? 1 : KP / 2;      // feature blocks; a lane's loads of K for 16 tokens
@@ -860,7 +860,7 @@ __device__ __forceinline__ float weight_of(float t, float inv) {
   return SOFTMAX ? __builtin_amdgcn_exp2f(t) : fabsf(t * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-t))) * inv;
 }
 
-// From the scores that the attention kernel left, a token to a lane: units of 256 tokens.  64 users of one row over 8192 keys and 8 heads 6.8 us (16.8 MB of scores); from K again
+// From the scores that the attention kernel left, a token to a lane: units of 256 tokens.  64 users of one row over 8192 keys and 8 heads 5.9 us (16.8 MB of scores); from K again
 // the same read 268 MB.
 template <bool SOFTMAX, int USERS>
 __global__ __launch_bounds__(256) void weigh8_saved_kernel(WeighParams<USERS> p) {
