@@ -151,6 +151,21 @@ def test_kernels_of_few_and_of_many_rows_and_users(d, heads, dtype, form):
 
 
 @pytest.mark.parametrize("form", ["silu", "softmax"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d,heads", [(256, 8), (512, 8), (1024, 8)])
+def test_many_rows_whose_ranges_are_arrays(d, heads, dtype, form):
+    """Items of 32 rows whose tiles follow from row_first and row_end, of few users and of many."""
+    for lens, rows, check in (([700, 650, 70, 640], [610, 600, 605, 640], [0, 2, 3]), ([300 + 13 * u for u in range(26)], [70 + u % 7 for u in range(26)], [0, 13, 25])):
+        c = Case(d, heads, dtype, form, lens, rows, seed=d + len(lens) + 1, check=check)
+        n = sum(rows)
+        first = c.rng.integers(-10, 500, n)
+        end = first + c.rng.integers(-5, 200, n)      # (some of them empty)
+        c.check(*c.call(cap=15.0, prefix=[3] * len(lens), first=first, end=end, weigh=True))
+        c.check(*c.call(causal=True, bias=True, window=120, first=sessions(c), weigh=True))
+        c.check(c.call(causal=True, end=c.rng.integers(0, 700, n)))
+
+
+@pytest.mark.parametrize("form", ["silu", "softmax"])
 def test_launches_that_do_not_keep_the_codes(form):
     """Few rows over more than the caches hold."""
     lens, rows = [8200] * 66, [1] * 65 + [2]
