@@ -163,6 +163,8 @@ def test_many_rows_whose_ranges_are_arrays(d, heads, dtype, form):
         c.check(*c.call(cap=15.0, prefix=[3] * len(lens), first=first, end=end, weigh=True))
         c.check(*c.call(causal=True, bias=True, window=120, first=sessions(c), weigh=True))
         c.check(c.call(causal=True, end=c.rng.integers(0, 700, n)))
+        key_pos = [np.cumsum(c.rng.integers(1, 4, m)) for m in lens]      # rows far from each other, caps that take the series
+        c.check(*c.call(cap=300.0, bias=True, end=end, key_pos=key_pos, row_pos=c.rng.integers(-500, 3000, n), weigh=True))
 
 
 @pytest.mark.parametrize("form", ["silu", "softmax"])
@@ -231,11 +233,12 @@ def test_large_scores_infinities_and_caps():
 
 
 @pytest.mark.parametrize("form", ["silu", "softmax"])
-@pytest.mark.parametrize("d,heads,dtype", [(256, 4, "bf16"), (128, 4, "fp16"), (256, 2, "fp16")])
-def test_nan_reaches_the_rows_that_see_it_only(d, heads, dtype, form):
+@pytest.mark.parametrize("d,heads,dtype,n,m", [(256, 4, "bf16", 250, 100), (128, 4, "fp16", 250, 100), (256, 2, "fp16", 250, 100), (512, 8, "bf16", 1200, 2100), (256, 8, "fp16", 1200, 2100),
+                                               (1024, 8, "bf16", 1200, 2100)])
+def test_nan_reaches_the_rows_that_see_it_only(d, heads, dtype, n, m, form):
     """NaN in K or V of one token of one head: rows that do not see the token, by a window, a session or their own place, stay as they are, and so do the other tokens' weights of
     rows that do not see it."""
-    n, m, at, dh = 250, 100, 170, d // heads
+    at, dh = 170, d // heads
     for what in "kv":
         c = Case(d, heads, dtype, form, [n], [m], seed=41)
         first = c.rng.integers(100, 240, m)
