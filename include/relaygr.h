@@ -376,7 +376,8 @@ typedef struct {
  * stays): the `first` ones, the `recent` last ones, and of the others those with the largest weight, ties going to the lowest place; NaN is below every
  * number.  They become the first tokens of the entry, or of to[u], in their order and in every layer, quantised anew from the values their codes stand for; the tokens behind
  * them in their last block become zero, and an entry of which nothing stays is left as it is.  A token keeps the position its K was made for: pass on `position`.  weight_out may be weight,
- * and position_out position, with out_off = token_off; outputs must not overlap otherwise.  No context, no scratch: it may be captured.  Errors as in the calls on an 8-bit pool;
+ * and position_out position, with out_off = token_off; outputs must not overlap otherwise.  Nothing is written behind what stays: where weight_out is weight, the places from what stays up to
+ * key_len still hold weights of before, and have to be cleared before tokens that are written there have their weights added up.  No context, no scratch: it may be captured.  Errors as in the calls on an 8-bit pool;
  * RELAYGR_EINVAL also if more tokens are to stay than there are or than to[u] holds, if first + recent are more than that where any leave, and if an entry
  * would be written twice or written by one user and read by another. */
 int  relaygr_kv_pool_evict(relaygr_kv_pool* pool, const relaygr_kv_rows* rows, const relaygr_kv_eviction* eviction, void* hip_stream);

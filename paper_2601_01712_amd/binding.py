@@ -663,7 +663,8 @@ def relaygr_kv_pool_evict(pool: KvPool, rows: KvRows, weight: torch.Tensor, toke
                           position: Optional[torch.Tensor] = None, position_out: Optional[torch.Tensor] = None, out_off: Optional[Sequence[int]] = None,
                           stream=None) -> torch.Tensor:
     """Evicts the tokens with the least weight: rows.row_off says how many of the first rows.key_len tokens of each entry stay.  Returns `kept` (int32
-    [rows.n_rows], made here if not given): the places of those that stay."""
+    [rows.n_rows], made here if not given): the places of those that stay.  Where weight_out is weight, the places behind them still hold weights of
+    before: clear them before tokens that are written there have theirs added up."""
     guard = _kv_guard(pool, stream)
     if guard is not None:
         with guard:
