@@ -322,8 +322,8 @@ typedef struct {
   int32_t  reserved;
   uint64_t turns[64];         /* of pair i: the fraction of a turn per position, times 2^64 (a caller may set frequencies of its own) */
 } relaygr_rope;
-/* Fills *out.  RELAYGR_EINVAL for a dim that is not even and between 2 and 128, an unknown layout, a base or factor that is not positive and finite, or
- * original_len > 0 without low < high. */
+/* Fills *out, turns to the nearest 2^-64.  RELAYGR_EINVAL for a dim that is not even and between 2 and 128, an unknown layout, a base or factor that is not positive and
+ * finite, original_len > 0 without low < high, or a frequency of 2^48 turns a position or more. */
 int  relaygr_rope_init(relaygr_rope* out, int32_t dim, int32_t layout, double base, double factor, int32_t original_len, double low, double high, float gain);
 /* Turns rows of q, and of k unless it is null, by the rows' positions (DEVICE int32 [n_rows]; any value, negative ones too): a' = gain (a cos - b sin),
  * b' = gain (a sin + b cos), the head's features from `dim` on copied; transposed != 0: by the opposite angle, which is the gradient of that, and undoes it where gain

@@ -11,6 +11,55 @@
 
 using namespace relaygr;
 
+namespace {
+
+// Numbers hi + lo of some 120 bits, for frequencies: of one that turns often only the fraction of a turn counts, and positions multiply what is lost of it.  (64 bits
+// alone were off by 2^-48 of a turn at a base of 1e-6, 6e-5 in the angle at position 2^31.)
+struct Wide { long double hi, lo; };
+Wide sum(long double a, long double b) {
+  const long double s = a + b, x = s - a;
+  return {s, (a - (s - x)) + (b - x)};
+}
+Wide operator+(const Wide& a, const Wide& b) {
+  const Wide s = sum(a.hi, b.hi);
+  return sum(s.hi, s.lo + (a.lo + b.lo));
+}
+// (halves of 32 bits, whose products are exact)
+Wide halves(long double x) {
+  const long double y = x * 0x100000001p0L, hi = y - (y - x);
+  return {hi, x - hi};
+}
+Wide operator*(const Wide& a, const Wide& b) {
+  const long double p = a.hi * b.hi;
+  const Wide x = halves(a.hi), y = halves(b.hi);
+  const long double rest = ((x.hi * y.hi - p) + x.hi * y.lo + x.lo * y.hi) + x.lo * y.lo;
+  return sum(p, rest + (a.hi * b.lo + a.lo * b.hi));
+}
+Wide operator/(const Wide& a, const Wide& b) {
+  const long double q = a.hi / b.hi;
+  const Wide rest = a + b * Wide{-q, 0};
+  return sum(q, (rest.hi + rest.lo) / b.hi);
+}
+
+// base^(-1 / n), 0 < n <= 64: with base = m 2^e the n-th root of 2^r / m, times 2^k, k n + r = -e; the root from powl's (off by some 2^-62), of which the n-th power is off by c:
+// times (1 + c)^(1 / n), to its square.
+Wide root_of(double base, int n) {
+  int e;
+  const double m = frexp(base, &e);
+  int k = -e / n, r = -e % n;
+  if (r < 0) { r += n; --k; }
+  const Wide of = Wide{ldexpl(1, r), 0} / Wide{m, 0};
+  const long double root = powl(of.hi, 1.0L / n);
+  Wide x = {root, 0}, power = {1, 0};
+  for (int j = n; j > 0; j >>= 1, x = x * x)
+    if (j & 1) power = power * x;
+  const long double c = (of / power + Wide{-1, 0}).hi / n;
+  const Wide f = sum(root, root * (c - (n - 1) / 2.0L * c * c));
+  return {ldexpl(f.hi, k), ldexpl(f.lo, k)};
+}
+
+}  // namespace
+
 extern "C" int relaygr_rope_init(relaygr_rope* out, int32_t dim, int32_t layout, double base, double factor, int32_t original_len, double low, double high,
                                  float gain) {
   static const char* what = "rope_init";
@@ -21,18 +70,21 @@ extern "C" int relaygr_rope_init(relaygr_rope* out, int32_t dim, int32_t layout,
   if (original_len < 0 || (original_len > 0 && (!isfinite(low) || !isfinite(high) || !(low < high)))) return fail(RELAYGR_EINVAL, "%s: original length, low or high", what);
   *out = relaygr_rope();
   out->dim = dim; out->layout = layout; out->gain = gain;
-  const long double turn = 6.283185307179586476925286766559L;
-  for (int i = 0; i < dim / 2; ++i) {
-    const long double f = powl((long double)base, -2.0L * i / dim);
-    long double keep = 0;
+  const Wide per_turn = {0xa2f9836e4e44152ap-66L, -0x3d8a82e0acb223fp-130L};      // 1 / 2 pi
+  const Wide step = root_of(base, dim / 2), shorter = Wide{1, 0} / Wide{factor, 0};
+  Wide frequency = {1, 0};
+  for (int i = 0; i < dim / 2; ++i, frequency = frequency * step) {
+    Wide turns = frequency * per_turn, keep = {0, 0};
     if (original_len > 0) {
-      keep = (original_len * f / turn - low) / ((long double)high - low);
-      keep = keep < 0 ? 0 : keep > 1 ? 1 : keep;
+      keep = (turns * Wide{(long double)original_len, 0} + Wide{-(long double)low, 0}) / sum(high, -(long double)low);
+      keep = keep.hi < 0 ? Wide{0, 0} : keep.hi >= 1 ? Wide{1, 0} : keep;
     }
-    const long double turns = f * (keep + (1 - keep) / factor) / turn;
-    if (!isfinite(turns)) return fail(RELAYGR_EINVAL, "%s: a frequency beyond any", what);
-    const long double scaled = roundl(ldexpl(turns - floorl(turns), 64));
-    out->turns[i] = scaled >= 0x1p64L ? 0 : (uint64_t)scaled;
+    turns = turns * (keep + (Wide{1, 0} + Wide{-keep.hi, -keep.lo}) * shorter);
+    if (!(turns.hi < 0x1p48L)) return fail(RELAYGR_EINVAL, "%s: a frequency of %Lg turns a position", what, turns.hi);      // (beyond, its fraction would be known to fewer than 64 bits)
+    const Wide fraction = sum(turns.hi - floorl(turns.hi), turns.lo);
+    const long double scaled = ldexpl(fraction.hi, 64), whole = floorl(scaled);
+    const long double rounded = whole + floorl(scaled - whole + ldexpl(fraction.lo, 64) + 0.5L);
+    out->turns[i] = rounded >= 0x1p64L ? 0 : (uint64_t)(rounded < 0 ? rounded + 0x1p64L : rounded);
   }
   return RELAYGR_OK;
 }

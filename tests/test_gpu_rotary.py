@@ -1,9 +1,12 @@
 """Rotary positions against the formula in extended precision."""
+import decimal
+
 import numpy as np
 import pytest
 import torch
 
 import paper_2601_01712_amd as rg
+from test_rotary_host import exact_turns
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -96,6 +99,22 @@ def test_far_and_negative_positions_scaled_frequencies_and_gain(dtype):
         for gain in (1.0, 1.139):
             got = rg.relaygr_rotary(cfg, rg.Rope(dh, gain=gain, **kw), torch.from_numpy(pos).to(DEV), q.to(DEV))
             check(got, *rotate(q64.reshape(-1, heads, dh), pos, dh, "half", frequencies(dh, **kw), gain=float(np.float32(gain))), dtype, dh)
+
+
+@pytest.mark.parametrize("kw", [dict(base=1e-6), dict(base=1e-4, factor=1e-4), dict(base=10000.0, factor=0.1)])
+def test_pairs_that_turn_many_times_a_position(kw):
+    """Angles from fractions of a turn to 80 digits: of far positions too, nothing is lost but the fraction's own rounding, 2^-65 of a turn a position."""
+    d, heads, dh = 128, 2, 64
+    cfg = rg.make_config(1, d, heads, "fp32")
+    pos = np.array([0, 1, -1, 12345, 2 ** 24 + 1, 2 ** 31 - 1, -2 ** 31], np.int32)
+    q, q64 = rows(np.random.default_rng(17), len(pos), d, "fp32")
+    with decimal.localcontext(decimal.Context(prec=80)):
+        t = 2 * np.pi * np.array([[float(int(p) * exact_turns(dh, i, **kw) % 1) for i in range(dh // 2)] for p in pos])[:, None]
+    x = q64.reshape(-1, heads, dh)
+    a, b = x[..., :dh // 2], x[..., dh // 2:]
+    want = np.concatenate([a * np.cos(t) - b * np.sin(t), a * np.sin(t) + b * np.cos(t)], -1)
+    off = np.tile((np.abs(a) + np.abs(b)) * (2.0 ** -22 + 2 * np.pi * 2.0 ** -34), 2)      # (sine and cosine as in rotate; the fraction's rounding at 2^31 positions)
+    check(rg.relaygr_rotary(cfg, rg.Rope(dh, **kw), torch.from_numpy(pos).to(DEV), q.to(DEV)), want, off, "fp32", dh)
 
 
 @pytest.mark.parametrize("layout,dim", [("half", 64), ("half", 20), ("half", 48), ("interleaved", 64), ("interleaved", 22)])

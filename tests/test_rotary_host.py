@@ -1,5 +1,6 @@
 """Rotary positions without a GPU: frequencies as they are kept, and every refusal that is made before anything is enqueued."""
 import ctypes as C
+import decimal
 import math
 
 import numpy as np
@@ -79,3 +80,35 @@ def test_refused_calls():
 def test_binding_refuses_tensors_on_the_host():
     with pytest.raises(rg.RelayGRError):
         rg.relaygr_rotary(rg.make_config(1, 128, 2, "bf16"), rg.Rope(64), torch.zeros(1, dtype=torch.int32), torch.zeros(1, 128, dtype=torch.bfloat16))
+
+
+def exact_turns(dim, i, base, factor=1.0, original_len=0, low=1.0, high=32.0):
+    """Turns a position of pair i, to 80 digits."""
+    with decimal.localcontext(decimal.Context(prec=80)):
+        tau = 2 * decimal.Decimal("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803482534211706798")
+        turns = decimal.Decimal(base) ** (decimal.Decimal(-2 * i) / dim) / tau
+        keep = decimal.Decimal(0)
+        if original_len:
+            keep = (original_len * turns - decimal.Decimal(low)) / (decimal.Decimal(high) - decimal.Decimal(low))
+            keep = min(max(keep, decimal.Decimal(0)), decimal.Decimal(1))
+        return turns * (keep + (1 - keep) / decimal.Decimal(factor))
+
+
+@pytest.mark.parametrize("kw", [dict(base=10000.0), dict(base=500000.0), dict(base=0.25), dict(base=1e-4), dict(base=1e-6), dict(base=1e-6, factor=3.7), dict(base=1e-12), dict(base=1e300),
+                                dict(base=10000.0, factor=0.1), dict(base=1e-4, factor=1e-4), dict(base=1.0, factor=1e-13), dict(base=7.3, factor=40.0, original_len=2048, low=0.5, high=3.5),
+                                dict(base=1e-3, factor=1e-5, original_len=100, low=1.0, high=2000.0), dict(base=10000.0, factor=4.0, original_len=4096, low=100.0, high=100.0 + 1e-9)])
+@pytest.mark.parametrize("dim", [2, 6, 20, 64, 126, 128])
+def test_frequencies_keep_all_bits_of_their_fraction(dim, kw):
+    """Also where a position turns a pair many times, of which only the fraction is kept: half of 2^-64 by its rounding, and as much for everything before it."""
+    rope = rg.Rope(dim, **kw)
+    for i in range(dim // 2):
+        with decimal.localcontext(decimal.Context(prec=80)):
+            want = exact_turns(dim, i, **kw) % 1 * 2 ** 64
+            off = abs(decimal.Decimal(rope.c.turns[i]) - want)
+            assert min(off, 2 ** 64 - off) <= 1, (i, off)
+
+
+def test_frequencies_beyond_the_bits_are_refused():
+    lib, out = rg.load_library(), B.RopeC()
+    for base, factor, code in ((1e-300, 1.0, rg.RELAYGR_EINVAL), (5e-324, 1e-300, rg.RELAYGR_EINVAL), (1.0, 2.0 ** -51, rg.RELAYGR_EINVAL), (1.0, 2.0 ** -50, 0), (1e308, 1e308, 0)):
+        assert lib.relaygr_rope_init(C.byref(out), 64, 0, base, factor, 0, 1.0, 32.0, 1.0) == code, (base, factor)
