@@ -576,6 +576,13 @@ def relaygr_rotary(cfg: ModelConfigC, rope: Rope, positions: torch.Tensor, q: to
     return q_out if k is None else (q_out, k_out)
 
 
+def _int32(what: str, x) -> int:
+    """x, unless the struct's 32 bits would hold another number."""
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise RelayGRError(RELAYGR_EINVAL, f"{what}: {x} is beyond 32 bits")
+    return x
+
+
 def _host_vector(what: str, x, dtype, n: Optional[int] = None):
     a = np.array(x, dtype=dtype)
     if a.ndim != 1 or (n is not None and a.size != n):
@@ -594,6 +601,9 @@ class Scoring:
                  row_first: Optional[torch.Tensor] = None, row_end: Optional[torch.Tensor] = None, row_position: Optional[torch.Tensor] = None,
                  key_position: Optional[torch.Tensor] = None, token_off: Optional[Sequence[int]] = None):
         self.slopes, self.row_first, self.row_end, self.row_position, self.key_position = slopes, row_first, row_end, row_position, key_position
+        if prefix is not None and np.size(prefix):     # (numpy would keep the low 32 bits of an array's wider elements)
+            _int32("Scoring: prefix", np.min(prefix))
+            _int32("Scoring: prefix", np.max(prefix))
         self.prefix = None if prefix is None else _host_vector("Scoring: prefix", prefix, np.int32)
         self.token_off = None if token_off is None else _host_vector("Scoring: token_off", token_off, np.int64)
         if key_position is not None and token_off is None:
@@ -601,8 +611,10 @@ class Scoring:
         self.tensors = [x for x in (("slopes", slopes, torch.float32), ("row_first", row_first, torch.int32), ("row_end", row_end, torch.int32),
                                     ("row_position", row_position, torch.int32), ("key_position", key_position, torch.int32)) if x[1] is not None]
         self.arrays = [x for x in (("prefix", self.prefix), ("token_off", self.token_off)) if x[1] is not None]
-        self.c = ScoringC(cap, window, None, None if self.prefix is None else self.prefix.ctypes.data_as(C.POINTER(C.c_int32)), None, None, None, None,
+        self.c = ScoringC(cap, _int32("Scoring: window", window), None, None if self.prefix is None else self.prefix.ctypes.data_as(C.POINTER(C.c_int32)), None, None, None, None,
                           None if self.token_off is None else self.token_off.ctypes.data_as(C.POINTER(C.c_int64)))
+        if cap != 0 and self.c.cap == 0:     # (0 would be no cap at all)
+            raise RelayGRError(RELAYGR_EINVAL, f"Scoring: a cap of {cap} is below what fp32 holds")
         self.ref = C.byref(self.c)
 
     def __setattr__(self, name, value):
@@ -674,7 +686,8 @@ def relaygr_kv_pool_evict(pool: KvPool, rows: KvRows, weight: torch.Tensor, toke
     out_off = None if out_off is None else _host_vector("kv_pool_evict: out_off", out_off, np.int64, n)
     to = None if to is None else _host_vector("kv_pool_evict: to", to, np.uint64, n)
     kept = torch.empty(rows.n_rows, dtype=torch.int32, device=device) if kept is None else kept
-    e = KvEvictionC(first, recent, None if to is None else to.ctypes.data, _vector("kv_pool_evict: weight", weight, torch.float32, device),
+    e = KvEvictionC(_int32("kv_pool_evict: first", first), _int32("kv_pool_evict: recent", recent), None if to is None else to.ctypes.data,
+                    _vector("kv_pool_evict: weight", weight, torch.float32, device),
                     _vector("kv_pool_evict: position", position, torch.int32, device), token_off.ctypes.data,
                     _vector("kv_pool_evict: kept", kept, torch.int32, device, rows.n_rows), _vector("kv_pool_evict: weight_out", weight_out, torch.float32, device),
                     _vector("kv_pool_evict: position_out", position_out, torch.int32, device),

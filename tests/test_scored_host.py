@@ -3,6 +3,7 @@ import ctypes as C
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2601_01712_amd as rg
 from paper_2601_01712_amd import binding as B
@@ -109,3 +110,26 @@ def test_scoring_is_what_it_was_made_with():
     s.prefix[:] = 7
     s.token_off += 1
     assert list(s.c.prefix[:2]) == [7, 7] and list(s.c.token_off[:2]) == [1, 11]
+
+
+@pytest.mark.parametrize("kw", [dict(cap=1e-50), dict(cap=-1e-50), dict(window=2 ** 32), dict(window=2 ** 31), dict(window=2 ** 32 + 5), dict(window=-2 ** 31 - 1), dict(prefix=np.array([2 ** 32 + 3])),
+                                dict(prefix=np.array([1, -2 ** 32])), dict(prefix=[2 ** 40]), dict(prefix=[5, 2 ** 70]), dict(prefix=np.array([2 ** 32 - 1], np.uint32))])
+def test_numbers_that_the_struct_would_hold_as_others_are_refused(kw):
+    with pytest.raises(rg.RelayGRError) as e:
+        rg.Scoring(**kw)
+    assert e.value.code == rg.RELAYGR_EINVAL
+
+
+def test_numbers_at_the_ends_of_their_types():
+    s = rg.Scoring(cap=2.0 ** -100, window=2 ** 31 - 1, prefix=np.array([2 ** 31 - 1, 0]))
+    assert s.c.cap == 2.0 ** -100 and s.c.window == 2 ** 31 - 1 and s.prefix.tolist() == [2 ** 31 - 1, 0]
+    assert rg.Scoring(prefix=[]).prefix.size == 0
+
+
+@pytest.mark.parametrize("kw", [dict(first=2 ** 32), dict(recent=2 ** 32 + 4), dict(first=-2 ** 32), dict(recent=2 ** 31)])
+def test_eviction_refuses_counts_beyond_their_type(monkeypatch, kw):
+    p = FakePool(rg.make_config(**CFG), pages=20)
+    p.slab = torch.zeros(0)
+    monkeypatch.setattr(B, "_kv_guard", lambda pool, stream: None)
+    with pytest.raises(rg.RelayGRError, match="beyond 32 bits"):
+        rg.relaygr_kv_pool_evict(p, rg.KvRows([rg.relaygr_kv_pool_alloc(p, 1, 100)], [0, 10], key_len=[100]), torch.zeros(100), [0], **kw)
