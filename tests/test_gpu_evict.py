@@ -134,6 +134,29 @@ def test_counts_ties_and_odd_weights(n):
     c.check(kept, [m], 0, n // 4)
 
 
+@pytest.mark.parametrize("kind", ["specials", "equal", "a step apart"])
+@pytest.mark.parametrize("n", [255, 256, 257, 1023, 1024, 1025, 2047, 2048, 2049, 4095, 4096, 4097, 5000, 33000])
+def test_large_counts_of_ties_and_odd_weights(n, kind):
+    """Counts around the choosing's spans of tokens (1024 threads of four; 4096 tokens in registers, 32 768 in LDS), where ties lie in several of them."""
+    c = Case(128, 4, "bf16", [n], seed=n, layers=1, to_lens=[n])
+    rng = np.random.default_rng(n)
+    if kind == "specials":
+        w = rng.choice(np.array([0.0, -0.0, np.inf, -np.inf, np.nan, 1e-42, -1e-42, 1.0, -1.0, 3.4e38], np.float32), n)
+    elif kind == "equal":
+        w = np.full(n, 0.25, np.float32)
+    else:
+        w = np.float32(1.0) + np.arange(n, dtype=np.float32) % 7 * np.float32(2.0 ** -23)
+    c.w[c.token_off[0]:c.token_off[0] + n] = w
+    for m in sorted({m for m in (129, n // 2, n // 2 + 1, 1024, 1025, 4096, n - 1, n) if m <= n}):
+        for first, recent in ((0, 0), (1, 0), (0, 1), (1, m // 3), (m // 2, m - m // 2), (m // 2, m - m // 2 - 1)):
+            kept = c.evict([m], first, recent, to=c.to)
+            want = choose(w, m, first, recent)
+            assert np.array_equal(kept.cpu().numpy(), want), (m, first, recent)
+            assert np.array_equal(c.weight_out.cpu().numpy()[:m], w[want], equal_nan=True) and np.array_equal(c.pos_out.cpu().numpy()[:m], c.mine(c.pos, 0)[want])
+    c.check(c.evict([m - 1], 0, n // 4, to=c.to), [m - 1], 0, n // 4, to=c.to)
+    c.check(c.evict([m - 1], 0, n // 4), [m - 1], 0, n // 4)
+
+
 @pytest.mark.parametrize("n", [4095, 4096, 4097, 16385, 32768, 32769, 40001])
 def test_long_entries(n):
     """Lengths around what the choosing holds in registers and in LDS: weights of many values and of few, whose ties lie in several spans of tokens; weights and positions over themselves."""
