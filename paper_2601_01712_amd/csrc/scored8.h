@@ -3,9 +3,11 @@
 //     t_ij = alpha <q_i, k_j>,   t <- cap tanh(t / cap),   t <- t - slope_h |p_i - p_j|
 //     softmax form  w_ij = exp(t_ij) / sum_j exp(t_ij)        SiLU form  w_ij = SiLU(t_ij) / n_i, n_i the tokens that the row sees
 //     o_i = sum_j w_ij v_j        (0 where n_i = 0)           W_j <- W_j + sum over heads and rows of |w_ij|
-// Products, operand layouts and roundings are those of attend8.h; scores are in units of ln 2.  cap tanh(t / cap) = cap - 2 cap / (1 + exp(2 t / cap)): an exp2 and a
-// reciprocal, off by 2^-23 of the cap at most, and nothing where the score is beyond fp32.  Caps above kCapSeries, where that would be felt in small scores, take the
-// power series of tanh up to 0.3 as well.
+// Products, operand layouts and roundings are those of attend8.h; scores are in units of ln 2.  cap tanh(t / cap) = cap - 2 cap / (1 + e), e = exp(2 t / cap): an exp2 and a
+// reciprocal, right also where e is beyond fp32.  In units of 2^-23, with exp2 and the reciprocal an ulp off: exp2 and its argument |2 t / cap| + 1 of e, the sum 1/2 and the reciprocal 1 of
+// themselves, in all at most 1.64 of 1 / (1 + e), which is twice as much of the cap; the factors and the last sum 1/2 each: 4.3, 2^-20.8 of the cap (2.2 with both rounded right, 3.2 with both an ulp off,
+// over a million scores).  Up to a cap of kCapSeries that is 7e-5 of a weight, a seventh of its rounding to fp16; above, where it would be felt in small scores, the
+// power series of tanh is taken up to 0.3 as well.
 //
 // Tokens' weights need the sums that a row ends with, so that a second kernel adds them up: from the scores, where the first left them in scratch (few rows: 4 bytes
 // a score instead of d_head codes of K), or from K and q again.  It adds in one order, one workgroup to a token: no atomics.

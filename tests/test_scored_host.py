@@ -133,3 +133,20 @@ def test_eviction_refuses_counts_beyond_their_type(monkeypatch, kw):
     monkeypatch.setattr(B, "_kv_guard", lambda pool, stream: None)
     with pytest.raises(rg.RelayGRError, match="beyond 32 bits"):
         rg.relaygr_kv_pool_evict(p, rg.KvRows([rg.relaygr_kv_pool_alloc(p, 1, 100)], [0, 10], key_len=[100]), torch.zeros(100), [0], **kw)
+
+
+@pytest.mark.parametrize("cap", [2.0 ** -100, 1.0, 30.0, 50.0, 128.0])
+def test_the_bound_of_capped_scores(cap):
+    """cap - 2 cap / (1 + exp(2 t / cap)) in 32 bits, with exp2 and the reciprocal off by an ulp either way: within 4.3 * 2^-23 of the cap."""
+    rng, f, per_ln2 = np.random.default_rng(0), np.float32, 1.4426950408889634
+    mul, add, cap_mul = f(-2 * cap * per_ln2), f(cap * per_ln2), f(2 * per_ln2 / cap)
+    t = (np.concatenate([rng.uniform(-12, 12, 50000), rng.uniform(-2, 2, 50000), np.exp(rng.uniform(-20, 3, 20000))]) * cap / 2).astype(f)
+    want = cap * np.tanh(t.astype(np.float64) / cap) * per_ln2
+    for exp_off in (0, 1, -1):
+        for rcp_off in (0, 1, -1):
+            e = np.exp2((t * cap_mul).astype(np.float64)).astype(f)
+            e = np.nextafter(e, f(exp_off * np.inf)) if exp_off else e
+            r = (1.0 / (f(1) + e).astype(np.float64)).astype(f)
+            r = np.nextafter(r, f(rcp_off * np.inf)) if rcp_off else r
+            got = (mul.astype(np.float64) * r + add).astype(f)
+            assert np.abs(got - want).max() <= 4.3 * 2.0 ** -23 * cap * per_ln2
