@@ -66,7 +66,9 @@ template <> struct RotaryType<F16> : RotaryType16<F16> {};
 
 // A lane's unit of a row, in `heads_per` heads of every array: the angles are worked out once for all of them, while the first four heads are on their way.  A head's lanes are in
 // one wavefront and read all that they turn before they write any of it, so that `out` may be `in`.  What bounds it is HBM, or the launch: q and k of 65 536 rows of 512 bf16, 268 MB,
-// 53 us (5.1 TB/s; a copy of 1 GiB reaches 5.0), of 16 384 15.9; one row 3.8.
+// 53 us (5.1 TB/s; a copy of 1 GiB reaches 5.0), of 16 384 15.9; one row 3.8.  Half-layout pairs that are no 16-byte pieces (kRotaryOdd: `dim` / 2 not a multiple of 8, of 4 in fp32) take each
+// partner by a load of its own, and these loads bound it: 60 of 64 features of the 65 536 rows 110 us where 64 of 64 take 46 on the same card, of 2048 rows 12.1 and 4.5; in fp32, at half as many
+// of them for a byte, 104 and 106.
 template <class T, RotaryUnit UNIT>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   using R = RotaryType<T>;

@@ -632,7 +632,8 @@ __global__ __launch_bounds__(kAttendWaves * 64, DH == 128 ? 2 : 3) void scored8_
 //     (d_head 32: a chunk's halves are lanes' 8 bytes)
 //   V: the chunk of feature l16 of 16, token half kb, lane half g holds these very tokens, the first eight bytes those of T = 0, 1
 // What bounds it is HBM, or for single rows the chain of loads: 128 users of one row over 8192 keys, d = 512, bias, 162 us (1.07 GB, 6.7 TB/s), 201 with the scores
-// kept, whose 33.5 MB cost the same in whatever pieces they are stored; one row over 2048, d = 256, 8.2.
+// kept, whose 33.5 MB cost the same in whatever pieces they are stored; one row over 2048, d = 256, 8.2.  All arrays are in registers but two words (12 bytes of scratch) of the
+// softmax form with a bias at d_head 64 for few users.
 template <typename H, int DH, bool SOFTMAX, bool BIAS, bool ONCE, int USERS>
 __global__ __launch_bounds__(kAttendWaves * 64, DH == 128 ? 2 : 4) void scored8_few_kernel(ScoredParams<USERS> p) {
   constexpr int KP = DH / 32, FB = DH / 16, KL = DH < 64 ? 1 : KP / 2;      // feature blocks; a lane's loads of K for 16 tokens
@@ -901,7 +902,9 @@ __global__ __launch_bounds__(256) void weigh8_saved_kernel(WeighParams<USERS> p)
 
 // From K and q again: a workgroup to a tile, whose wavefronts share the user's (head, row block) pairs and add up over them in registers; the next pair's rows are on their
 // way while one is worked on.  What bounds it is the vector ALU, 14 instructions a score: 32 users of 200 to 1000 rows over about 4096 keys, d = 512, cap and bias (561 M scores) 278 us, the users
-// of most rows first (334 in another order, the ALU issuing in 87 % of the units' cycles); eight wavefronts a workgroup took 456 where four took 394.
+// of most rows first (334 in another order, the ALU issuing in 87 % of the units' cycles); eight wavefronts a workgroup took 456 where four took 394.  With a bias at d_head 64 the 168 registers of
+// three wavefronts a SIMD do not hold everything: 13 words (SiLU form) or 16 are in scratch.  Rows are asked for their ranges after their products, so that masks save the scores and not the
+// products: 16 users of 200 rows over 8192 keys, d = 512, 73 us (of a call's 162) if all see all, 75 with a window of 2000 or 81 with sessions of 400, where the attention itself falls from 89 to 29 and 16.
 constexpr int kWeighWaves = 4;
 template <typename H, int DH, bool SOFTMAX, bool BIAS, int USERS>
 __global__ __launch_bounds__(kWeighWaves * 64, DH == 128 ? 2 : 3) void weigh8_kernel(WeighParams<USERS> p) {
